@@ -345,6 +345,119 @@ typedef struct {
 } fd_unit_rates;
 fd_status fd_unit_peaks(void* scratch_dev, size_t scratch_bytes, void* cuda_stream, fd_unit_rates* out_host);
 
+/* ------------------------------------------------------------------ kept keys and values, attended to by new tokens
+ * The operators below are the softmax relatives of the products above: new rows against kept rows (fd_nystrom) with
+ * weights exp(scale q.k) that every row normalises to 1, and the column sums of those weights (fd_degree).  The kept rows
+ * live in pages of a pool.  They need no fd_ctx, take their stream per call and hold no device memory between calls.
+ *
+ * Element types: FD_BF16 and FD_FP16 (FD_FP32: fd_rotary only).  Scores, softmax statistics, sums and weights are fp32; a
+ * softmax weight is rounded to the element type as an operand of the product with the values, results once at the end.
+ * Heads: a tensor of heads is [token][head][head_dim] with unit stride inside a head; the other strides are free.
+ * Pages: token t of a sequence is row t % page_size of the pool's page table[t / page_size]; page_size is a multiple of 8.
+ * Lengths: sequence i has kv_len[i] tokens in the cache, the q_start[i + 1] - q_start[i] new ones among them, at the end; the new
+ *   tokens of all sequences follow each other in q, k, v and out.  Rows from q_start[batch] on (padding) are neither read into a result nor written.
+ *   All three arrays are read on the device, so a captured call takes its lengths at replay; total_q, max_new and max_len are
+ *   upper bounds that size the launch.  A page number outside the pool, or a length outside [0, min(max_len,
+ *   max_pages * page_size)], is never followed: the tokens count as zeros (not written by appends), the length is
+ *   clamped, and fd_kv_synchronize reports FD_ERR_INVALID.
+ * Positions: angles are taken in fp64 as position * freqs[i] and reduced there, so far positions lose nothing.
+ * Masks: new token i of a sequence stands at slot p = kv_len - new + i.  Causal: it sees slots <= p; window > 0: of these
+ *   the last `window`.  A row that sees nothing gets zeros and lse = -inf.  What a row does not see cannot reach it, not as an infinity or NaN either.
+ * Errors: an fd_status, with a message in errbuf (optional); argument errors are found before any launch.
+ * Repeats: the same call gives the same bits (no floating-point atomics).  Calls may be recorded into CUDA graphs. */
+typedef enum { FD_BF16 = 0, FD_FP16 = 1, FD_FP32 = 2 } fd_dtype;
+enum { FD_ROTARY_HALF = 0, FD_ROTARY_INTERLEAVED = 1 };
+enum { FD_ROTARY_PLAIN = 0, FD_ROTARY_LINEAR = 1, FD_ROTARY_BASE = 2, FD_ROTARY_RAMP = 3 };
+
+typedef struct {               /* [token][head][head_dim], strides in elements */
+    void*   p_dev;
+    int64_t token_stride, head_stride;
+    int32_t heads;
+} fd_heads;
+
+/* Frequencies of rotary positions, f_i = base^(-2 i / rot_dim), i < rot_dim / 2, and their scaling for long contexts:
+ *   LINEAR  f_i / factor;     BASE  base * factor^(rot_dim / (rot_dim - 2)) in place of base;
+ *   RAMP    f_i / factor where a coordinate turns at most `lo` times in original_len positions, f_i where it turns `hi` times or
+ *           more, linear in the number of turns between.
+ * freqs_host: rot_dim / 2 doubles. */
+fd_status fd_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                                double lo, double hi, double* freqs_host);
+
+/* Rotary positions: pairs (x_i, x_{i + rot_dim/2}) (HALF) or (x_2i, x_{2i+1}) (INTERLEAVED), i < rot_dim / 2, of every head are
+ * turned by positions[token] * freqs[i] and multiplied by `scale`; the coordinates from rot_dim on are copied.  inverse != 0 turns
+ * back: with the same scale that is the transpose, the gradient of x from the gradient of out.  out may be x itself; otherwise they
+ * must not overlap.  freqs_dev: rot_dim / 2 doubles. */
+fd_status fd_rotary(const fd_heads* x, const fd_heads* out, int32_t dtype, int32_t tokens, int32_t head_dim,
+                    const int32_t* positions_dev, const double* freqs_dev, int32_t rot_dim, int32_t layout, double scale,
+                    int32_t inverse, void* cuda_stream, char* errbuf, size_t errbuf_len);
+
+typedef struct {
+    void*   k_dev; void* v_dev;                /* pools; 16-byte aligned */
+    int64_t k_page_stride, k_token_stride, k_head_stride;     /* elements, multiples of 8 */
+    int64_t v_page_stride, v_token_stride, v_head_stride;
+    int32_t num_pages, page_size, heads, head_dim;            /* head_dim 64 or 128 */
+    int32_t dtype;                             /* FD_BF16 or FD_FP16 */
+    uint32_t* status_dev;                      /* 4 words, zeroed by the caller; what went wrong on the device */
+} fd_kv_desc;
+
+typedef struct {
+    const int32_t* table_dev; int64_t table_stride;           /* [batch][max_pages] */
+    const int32_t* kv_len_dev;                                /* [batch] */
+    const int32_t* q_start_dev;                               /* [batch + 1] */
+    int32_t batch, max_pages, total_q, max_new, max_len;
+} fd_kv_batch;
+
+/* A cache: what the calls below need to know of the pools, on the host alone.  It is not changed by calls, so several streams and
+ * threads may use it at once (on different pages).  The pools and status words stay the caller's. */
+typedef struct fd_kv fd_kv;
+fd_status fd_kv_create(fd_kv** out, const fd_kv_desc* desc, char* errbuf, size_t errbuf_len);
+void      fd_kv_destroy(fd_kv* kv);
+/* Waits for the stream, reads and clears the status words: FD_ERR_TIMEOUT (a bounded wait ran out), FD_ERR_INVALID (a page or
+ * length out of range), FD_OK. */
+fd_status fd_kv_synchronize(fd_kv* kv, void* cuda_stream);
+
+/* Writes the new tokens' keys, rotated, and values into their slots; q (optional) is rotated into q_out, which may be q.
+ * positions_dev null: no rotation (q must be null). */
+typedef struct {
+    fd_heads k, v, q, q_out;
+    const int32_t* positions_dev; const double* freqs_dev;
+    double  scale;
+    int32_t rot_dim, layout;
+} fd_kv_append_args;
+fd_status fd_kv_append(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_append_args* args, void* cuda_stream,
+                       char* errbuf, size_t errbuf_len);
+
+/* Attention of the new tokens over the cache: out = sum_j softmax_j(scale q.k_j) v_j over the slots each row sees; q_heads is a
+ * multiple (up to 128) of the cache's heads, query head h reads head h / (q_heads / heads).  lse_dev (optional): [total_q][q_heads], the natural
+ * logarithm of sum_j exp(scale q.k_j).  weights_out_dev (optional; [batch][heads][weights_stride] for both): weights_in + the sum over
+ * new tokens and query heads of the softmax weight a slot received, for slots below kv_len (others are left alone); weights_in
+ * null = zeros, and may be weights_out.  It needs lse_dev.  out must not overlap q. */
+typedef struct {
+    fd_heads q, out;
+    double   scale;
+    int32_t  causal, window;
+    float*   lse_dev;
+    const float* weights_in_dev; float* weights_out_dev; int64_t weights_stride;
+} fd_kv_attend_args;
+size_t    fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* batch, int32_t q_heads);
+fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_attend_args* args, void* workspace_dev,
+                       size_t workspace_bytes, void* cuda_stream, char* errbuf, size_t errbuf_len);
+
+/* Eviction: of every sequence longer than `keep`, each head keeps its first `first` tokens, its last `recent` ones and, of those between, the
+ * ones with the largest weights (of equal ones the earlier; a NaN counts as the smallest), `keep` in all and in their order: row r
+ * of the new cache is the old slot kept[r].  new_table: the pages they move to, either the same table as the batch's (in place) or pages that
+ * no sequence of the batch uses; ceil(keep / page_size) columns suffice.  kept_dev: [batch][heads][keep], -1 behind the last.  new_len_dev:
+ * [batch], may be kv_len.  weights_out_dev: the kept weights in their new order, zeros behind them up to kv_len; may be weights_in.
+ * q_start is not read. */
+typedef struct {
+    const float* weights_in_dev; float* weights_out_dev; int64_t weights_stride;
+    const int32_t* new_table_dev; int64_t new_table_stride; int32_t new_max_pages;
+    int32_t  keep, first, recent;
+    int32_t* kept_dev; int32_t* new_len_dev;
+} fd_kv_evict_args;
+fd_status fd_kv_evict(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_evict_args* args, void* cuda_stream,
+                      char* errbuf, size_t errbuf_len);
+
 const char* fd_status_string(fd_status st);
 const char* fd_last_error(const fd_ctx* ctx);
 int32_t     fd_version(void);

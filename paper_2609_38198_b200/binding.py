@@ -20,13 +20,17 @@ FD_ERR_PERRON_WALL, FD_ERR_UNSUPPORTED, FD_ERR_TIMEOUT, FD_ERR_NONFINITE, FD_ERR
 FD_PREC_FP32, FD_PREC_FAST = 0, 1
 FD_PATH_AUTO, FD_PATH_SIMT, FD_PATH_TC = 0, 1, 2
 FD_FLOW_VERTEX, FD_FLOW_PERRON_WALL, FD_FLOW_LEFT_EDGE, FD_FLOW_RIGHT_EDGE = 0, 1, 2, 3
+FD_BF16, FD_FP16, FD_FP32 = 0, 1, 2
+FD_ROTARY_HALF, FD_ROTARY_INTERLEAVED = 0, 1
+FD_ROTARY_PLAIN, FD_ROTARY_LINEAR, FD_ROTARY_BASE, FD_ROTARY_RAMP = 0, 1, 2, 3
 FLOW_OUTCOMES = {0: "VERTEX", 1: "PERRON_WALL", 2: "LEFT_EDGE", 3: "RIGHT_EDGE"}
 
 # Every symbol include/fd.h declares (checked by the CPU test-suite against the header).
 EXPORTS = [
     "fd_workspace_bytes", "fd_create", "fd_destroy", "fd_set_option", "fd_get_option", "fd_beta0", "fd_degree",
     "fd_apply", "fd_apply_general", "fd_synchronize", "fd_eigs", "fd_beta_flow", "fd_beta_flow_cascade", "fd_nystrom", "fd_ladder_start", "fd_scale_by_degree",
-    "fd_apply_general_static", "fd_unit_peaks", "fd_shard_rows", "fd_shard_exchange_bytes", "fd_set_shard", "fd_status_string", "fd_last_error", "fd_version", "fd_launch_count",
+    "fd_apply_general_static", "fd_unit_peaks", "fd_shard_rows", "fd_shard_exchange_bytes", "fd_set_shard", "fd_rotary_frequencies", "fd_rotary",
+    "fd_kv_create", "fd_kv_destroy", "fd_kv_synchronize", "fd_kv_append", "fd_kv_attend_bytes", "fd_kv_attend", "fd_kv_evict", "fd_status_string", "fd_last_error", "fd_version", "fd_launch_count",
 ]
 
 
@@ -54,6 +58,37 @@ class fd_flow_opts(Structure):
 
 class fd_cascade_stage(Structure):
     _fields_ = [("prec", c_int32), ("eta", c_double), ("tol", c_double)]
+
+
+class fd_heads(Structure):
+    _fields_ = [("p_dev", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64), ("heads", c_int32)]
+
+
+class fd_kv_desc(Structure):
+    _fields_ = ([("k_dev", c_void_p), ("v_dev", c_void_p)] + [(n, c_int64) for n in (
+        "k_page_stride", "k_token_stride", "k_head_stride", "v_page_stride", "v_token_stride", "v_head_stride")]
+        + [(n, c_int32) for n in ("num_pages", "page_size", "heads", "head_dim", "dtype")] + [("status_dev", c_void_p)])
+
+
+class fd_kv_batch(Structure):
+    _fields_ = [("table_dev", c_void_p), ("table_stride", c_int64), ("kv_len_dev", c_void_p), ("q_start_dev", c_void_p)] + [
+        (n, c_int32) for n in ("batch", "max_pages", "total_q", "max_new", "max_len")]
+
+
+class fd_kv_append_args(Structure):
+    _fields_ = [("k", fd_heads), ("v", fd_heads), ("q", fd_heads), ("q_out", fd_heads), ("positions_dev", c_void_p),
+                ("freqs_dev", c_void_p), ("scale", c_double), ("rot_dim", c_int32), ("layout", c_int32)]
+
+
+class fd_kv_attend_args(Structure):
+    _fields_ = [("q", fd_heads), ("out", fd_heads), ("scale", c_double), ("causal", c_int32), ("window", c_int32),
+                ("lse_dev", c_void_p), ("weights_in_dev", c_void_p), ("weights_out_dev", c_void_p), ("weights_stride", c_int64)]
+
+
+class fd_kv_evict_args(Structure):
+    _fields_ = [("weights_in_dev", c_void_p), ("weights_out_dev", c_void_p), ("weights_stride", c_int64),
+                ("new_table_dev", c_void_p), ("new_table_stride", c_int64), ("new_max_pages", c_int32), ("keep", c_int32),
+                ("first", c_int32), ("recent", c_int32), ("kept_dev", c_void_p), ("new_len_dev", c_void_p)]
 
 
 def _load() -> ctypes.CDLL:
@@ -97,6 +132,20 @@ def _load() -> ctypes.CDLL:
     lib.fd_apply_general_static.restype = c_int32
     lib.fd_unit_peaks.argtypes = [c_void_p, c_size_t, c_void_p, POINTER(fd_unit_rates)]
     lib.fd_unit_peaks.restype = c_int32
+    lib.fd_rotary_frequencies.argtypes = [c_int32, c_double, c_int32, c_double, c_double, c_double, c_double, POINTER(c_double)]
+    lib.fd_rotary.argtypes = [POINTER(fd_heads), POINTER(fd_heads), c_int32, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_int32,
+                              c_double, c_int32, c_void_p, c_char_p, c_size_t]
+    lib.fd_kv_create.argtypes = [POINTER(c_void_p), POINTER(fd_kv_desc), c_char_p, c_size_t]
+    lib.fd_kv_destroy.argtypes = [c_void_p]
+    lib.fd_kv_destroy.restype = None
+    lib.fd_kv_synchronize.argtypes = [c_void_p, c_void_p]
+    lib.fd_kv_append.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_append_args), c_void_p, c_char_p, c_size_t]
+    lib.fd_kv_attend_bytes.argtypes = [c_void_p, POINTER(fd_kv_batch), c_int32]
+    lib.fd_kv_attend_bytes.restype = c_size_t
+    lib.fd_kv_attend.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_attend_args), c_void_p, c_size_t, c_void_p, c_char_p, c_size_t]
+    lib.fd_kv_evict.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_evict_args), c_void_p, c_char_p, c_size_t]
+    for name in ("fd_rotary_frequencies", "fd_rotary", "fd_kv_create", "fd_kv_synchronize", "fd_kv_append", "fd_kv_attend", "fd_kv_evict"):
+        getattr(lib, name).restype = c_int32
     lib.fd_status_string.argtypes = [c_int32]
     lib.fd_status_string.restype = c_char_p
     lib.fd_last_error.argtypes = [c_void_p]
@@ -368,6 +417,234 @@ def fd_apply_general_static(X: torch.Tensor, beta: float, V: torch.Tensor, left=
     if st != FD_OK:
         raise FdError(st, err.value.decode())
     return Y
+
+
+# ---- kept keys and values, rotary positions (fd.h: "kept keys and values") ------------------------------------------
+_DTYPES = {torch.bfloat16: FD_BF16, torch.float16: FD_FP16, torch.float32: FD_FP32}
+_LAYOUTS = {"half": FD_ROTARY_HALF, "interleaved": FD_ROTARY_INTERLEAVED}
+_SCALINGS = {"none": FD_ROTARY_PLAIN, "linear": FD_ROTARY_LINEAR, "base": FD_ROTARY_BASE, "ramp": FD_ROTARY_RAMP}
+
+
+def _need(cond, what: str):
+    if not cond:
+        raise FdError(FD_ERR_INVALID, what)
+
+
+def _need_tensor(t, dtype, dims: int, device, what: str):
+    _need(isinstance(t, torch.Tensor) and t.dtype == dtype and t.dim() == dims and t.device == device, f"{what}: a {dims}-d {dtype} tensor on {device}")
+
+
+def _heads(t: torch.Tensor, dtype, device, head_dim: int, tokens: int, what: str) -> fd_heads:
+    """[tokens, heads, head_dim] with unit stride inside a head; strides of single tokens and heads do not matter."""
+    _need_tensor(t, dtype, 3, device, what)
+    n, h, d = t.shape
+    st, sh, sd = t.stride()
+    _need(n == tokens and d == head_dim and (sd == 1 or d == 1), f"{what}: [{tokens}, heads, {head_dim}] with unit stride inside a head")
+    return fd_heads(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d, h)
+
+
+def _stream(device) -> c_void_p:
+    return c_void_p(torch.cuda.current_stream(device).cuda_stream)
+
+
+def _raise(st: int, err):
+    raise FdError(st, err.value.decode())
+
+
+def fd_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                          original_len: float = 0.0, lo: float = 1.0, hi: float = 32.0, device=None) -> torch.Tensor:
+    """Frequencies of rotary positions (rot_dim / 2 doubles) on `device`; scaling: "none", "linear", "base" or "ramp"."""
+    _need(scaling in _SCALINGS, f"scaling: one of {sorted(_SCALINGS)}")
+    out = (c_double * max(1, rot_dim // 2))()
+    st = lib.fd_rotary_frequencies(rot_dim, base, _SCALINGS[scaling], factor, original_len, lo, hi, out)
+    if st != FD_OK:
+        raise FdError(st, "rot_dim, base, factor or ramp out of range")
+    return torch.tensor(list(out), dtype=torch.float64, device=device)
+
+
+def _rotary_args(positions, freqs, tokens: int, device, layout: str):
+    _need_tensor(positions, torch.int32, 1, device, "positions")
+    _need_tensor(freqs, torch.float64, 1, device, "freqs")
+    _need(positions.shape[0] == tokens and positions.is_contiguous(), f"positions: {tokens} contiguous values")
+    _need(freqs.is_contiguous(), "freqs must be contiguous")
+    _need(layout in _LAYOUTS, f"layout: one of {sorted(_LAYOUTS)}")
+    return _LAYOUTS[layout]
+
+
+def fd_rotary(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, layout: str = "half", scale: float = 1.0,
+              inverse: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rotary positions of x [tokens, heads, head_dim] on the current stream; with `inverse` the transpose, which takes the gradient of the
+    result to the gradient of x.  `out` may be x."""
+    _need(isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 3 and x.dtype in _DTYPES, "x: a CUDA tensor [tokens, heads, head_dim] of bf16, fp16 or fp32")
+    tokens, _, d = x.shape
+    code = _rotary_args(positions, freqs, tokens, x.device, layout)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    hx, hy = _heads(x, x.dtype, x.device, d, tokens, "x"), _heads(y, x.dtype, x.device, d, tokens, "out")
+    err = ctypes.create_string_buffer(256)
+    with _on(x.device):
+        st = lib.fd_rotary(byref(hx), byref(hy), _DTYPES[x.dtype], tokens, d, positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0],
+                           code, scale, 1 if inverse else 0, _stream(x.device), err, 256)
+    if st != FD_OK:
+        _raise(st, err)
+    return y
+
+
+class KVBatch:
+    """The sequences of a call: page table [batch, pages], tokens in the cache (the new ones among them) [batch], first new token of each
+    [batch + 1], all int32 on the GPU and read there (a captured call takes their values at replay), and upper bounds of the new tokens in
+    all, of one sequence's new tokens and of a sequence's length."""
+
+    def __init__(self, page_table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor, total_q: int, max_new: int, max_len: int):
+        dev = page_table.device
+        _need(page_table.is_cuda, "page_table: a CUDA tensor")
+        _need_tensor(page_table, torch.int32, 2, dev, "page_table")
+        _need_tensor(kv_len, torch.int32, 1, dev, "kv_len")
+        _need_tensor(q_start, torch.int32, 1, dev, "q_start")
+        n = page_table.shape[0]
+        _need(page_table.stride(1) == 1 or page_table.shape[1] == 1, "page_table: unit stride inside a row")
+        _need(kv_len.shape[0] == n and q_start.shape[0] == n + 1 and kv_len.is_contiguous() and q_start.is_contiguous(),
+              f"kv_len: {n} contiguous values, q_start: {n + 1}")
+        self.device, self.total_q = dev, int(total_q)
+        self.page_table, self.kv_len, self.q_start = page_table, kv_len, q_start
+        self.batch, self.max_len = n, int(max_len)
+        self.struct = fd_kv_batch(page_table.data_ptr(), max(page_table.stride(0), page_table.shape[1]), kv_len.data_ptr(), q_start.data_ptr(), n,
+                                  page_table.shape[1], total_q, max_new, max_len)
+
+
+class KVCache:
+    """Keys and values in pages: two pools [page, token in page, head, head_dim] (any strides with unit stride inside a head, so a pool laid
+    out [page, head, token, head_dim] is passed transposed).  Calls run on the current stream and mirror the C entry points; workspaces are
+    taken from the current stream's allocator for each call, so calls on several streams and captured graphs share nothing but the pools."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
+        _need(isinstance(k_pages, torch.Tensor) and k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in (torch.bfloat16, torch.float16),
+              "k_pages: a CUDA tensor [page, token, head, head_dim] of bf16 or fp16")
+        dev = k_pages.device
+        _need_tensor(v_pages, k_pages.dtype, 4, dev, "v_pages")
+        _need(k_pages.shape == v_pages.shape and k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "k_pages, v_pages: equal shapes, unit stride inside a head")
+        self.device, self.dtype = dev, k_pages.dtype
+        self.k_pages, self.v_pages = k_pages, v_pages
+        pages, size, heads, d = k_pages.shape
+        self.heads, self.head_dim = heads, d
+        self._status = torch.zeros(4, dtype=torch.int32, device=dev)
+        desc = fd_kv_desc(k_pages.data_ptr(), v_pages.data_ptr(), *[t.stride(i) if t.shape[i] > 1 else t.shape[1] * t.shape[2] * d
+                                                                   for t in (k_pages, v_pages) for i in (0, 1, 2)],
+                          pages, size, heads, d, _DTYPES[k_pages.dtype], self._status.data_ptr())
+        h, err = c_void_p(), ctypes.create_string_buffer(256)
+        with _on(dev):
+            torch.cuda.current_stream(dev).synchronize()       # the status words are zero for every stream from here on
+            st = lib.fd_kv_create(byref(h), byref(desc), err, 256)
+        if st != FD_OK:
+            _raise(st, err)
+        self._h = h
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib.fd_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def synchronize(self):
+        """Waits for the current stream; raises FdError if a page number or length was out of range, or a bounded wait ran out."""
+        with _on(self.device):
+            st = lib.fd_kv_synchronize(self._h, _stream(self.device))
+        if st != FD_OK:
+            raise FdError(st, "a page number or a length was out of range" if st == FD_ERR_INVALID else "")
+
+    def _batch(self, batch: KVBatch):
+        _need(batch.device == self.device, f"the batch is on {batch.device}, the cache on {self.device}")
+        return byref(batch.struct)
+
+    def append(self, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor | None = None, freqs: torch.Tensor | None = None,
+               layout: str = "half", scale: float = 1.0, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
+        """Writes the new tokens' keys (rotated, if there are positions) and values into the cache; rotates q beside them and returns it."""
+        n, dev, dt, d = batch.total_q, self.device, self.dtype, self.head_dim
+        a = fd_kv_append_args(_heads(k, dt, dev, d, n, "k"), _heads(v, dt, dev, d, n, "v"))
+        if positions is not None:
+            a.layout = _rotary_args(positions, freqs, n, dev, layout)
+            a.positions_dev, a.freqs_dev, a.rot_dim = positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0]
+        a.scale = scale
+        if q is not None:
+            a.q = _heads(q, dt, dev, d, n, "q")
+            q_out = torch.empty(q.shape, dtype=dt, device=dev) if q_out is None else q_out
+            a.q_out = _heads(q_out, dt, dev, d, n, "q_out")
+        err = ctypes.create_string_buffer(256)
+        with _on(dev):
+            st = lib.fd_kv_append(self._h, self._batch(batch), byref(a), _stream(dev), err, 256)
+        if st != FD_OK:
+            _raise(st, err)
+        return q_out
+
+    def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, causal: bool = True, window: int = 0,
+               out: torch.Tensor | None = None, lse: torch.Tensor | None = None, weights: torch.Tensor | None = None,
+               weights_out: torch.Tensor | None = None):
+        """Returns (out, lse) for the new tokens' queries [total_q, query heads, head_dim]; scale defaults to head_dim^-1/2.  With `weights`
+        ([batch, heads, >= max_len] fp32) and / or `weights_out` (default: weights itself) the softmax weights that every cached token received are
+        added up: weights_out = weights (or 0) + their sum."""
+        n, dev, dt, d = batch.total_q, self.device, self.dtype, self.head_dim
+        hq = _heads(q, dt, dev, d, n, "q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=dt, device=dev)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
+        _need_tensor(lse, torch.float32, 2, dev, "lse")
+        _need(lse.shape == q.shape[:2] and lse.is_contiguous(), "lse: [total_q, query heads], contiguous")
+        a = fd_kv_attend_args(hq, _heads(out, dt, dev, d, n, "out"), d ** -0.5 if scale is None else scale, 1 if causal else 0, window or 0, lse.data_ptr())
+        if weights is not None or weights_out is not None:
+            weights_out = weights if weights_out is None else weights_out
+            for t in (weights, weights_out):
+                if t is not None:
+                    self._check_weights(t, batch)
+                    _need(t.stride() == weights_out.stride(), "weights and weights_out: equal strides")
+            a.weights_in_dev, a.weights_out_dev = _ptr(weights), weights_out.data_ptr()
+            a.weights_stride = weights_out.stride(1)
+        b, err = self._batch(batch), ctypes.create_string_buffer(256)
+        with _on(dev):
+            size = lib.fd_kv_attend_bytes(self._h, b, hq.heads)
+            ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+            st = lib.fd_kv_attend(self._h, b, byref(a), _ptr(ws), size, _stream(dev), err, 256)
+        if st != FD_OK:
+            _raise(st, err)
+        return out, lse
+
+    def _check_weights(self, t: torch.Tensor, batch: KVBatch):
+        _need_tensor(t, torch.float32, 3, self.device, "weights")
+        _need(t.shape[0] == batch.batch and t.shape[1] == self.heads and t.shape[2] >= batch.max_len and t.is_contiguous(),
+              f"weights: [{batch.batch}, {self.heads}, {batch.max_len} or more], contiguous")
+
+    def evict(self, batch: KVBatch, weights: torch.Tensor, keep: int, first: int = 0, recent: int = 0, new_table: torch.Tensor | None = None,
+              kept: torch.Tensor | None = None, new_len: torch.Tensor | None = None, weights_out: torch.Tensor | None = None):
+        """Every head keeps `keep` tokens of each longer sequence: the first, the recent and the heaviest of the others, in order, moved to
+        the front of the sequence's pages (or to new_table's).  Returns (kept slots [batch, heads, keep], new lengths, weights)."""
+        dev = self.device
+        self._check_weights(weights, batch)
+        weights_out = weights if weights_out is None else weights_out
+        self._check_weights(weights_out, batch)
+        _need(weights_out.stride() == weights.stride(), "weights and weights_out: equal strides")
+        table = batch.page_table if new_table is None else new_table
+        _need_tensor(table, torch.int32, 2, dev, "new_table")
+        _need(table.shape[0] == batch.batch and (table.stride(1) == 1 or table.shape[1] == 1), "new_table: [batch, pages], unit stride inside a row")
+        if kept is None:
+            kept = torch.empty((batch.batch, self.heads, max(keep, 0)), dtype=torch.int32, device=dev)
+        if new_len is None:
+            new_len = torch.empty(batch.batch, dtype=torch.int32, device=dev)
+        _need_tensor(kept, torch.int32, 3, dev, "kept")
+        _need_tensor(new_len, torch.int32, 1, dev, "new_len")
+        _need(tuple(kept.shape) == (batch.batch, self.heads, keep) and kept.is_contiguous(), f"kept: [{batch.batch}, {self.heads}, {keep}], contiguous")
+        _need(new_len.shape[0] == batch.batch and new_len.is_contiguous(), f"new_len: {batch.batch} contiguous values")
+        a = fd_kv_evict_args(weights.data_ptr(), weights_out.data_ptr(), weights.stride(1), table.data_ptr(), max(table.stride(0), table.shape[1]),
+                             table.shape[1], keep, first, recent, kept.data_ptr(), new_len.data_ptr())
+        err = ctypes.create_string_buffer(256)
+        with _on(dev):
+            st = lib.fd_kv_evict(self._h, self._batch(batch), byref(a), _stream(dev), err, 256)
+        if st != FD_OK:
+            _raise(st, err)
+        return kept, new_len, weights_out
 
 
 def fd_unit_peaks(device) -> dict:

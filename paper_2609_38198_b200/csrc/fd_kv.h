@@ -1,0 +1,92 @@
+// Internal declarations of the paged cache's operators (fd_kv.cu: entry points; fd_kv_rows.cu: rotary positions, append, eviction;
+// fd_kv_attend.cu: attention and its column sums).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "fd_internal.h"
+
+struct fd_kv {
+    fd_kv_desc d{};
+    int box_rows = 0;                // rows of a page that one TMA box takes: gcd(page_size, 128)
+    int device = 0, sm_count = 148;
+    CUtensorMap map_k, map_v;        // (coordinate, row of the page, head, page)
+};
+
+namespace fd {
+namespace kv {
+
+// Bits of a cache's first status word; the second holds the code of a wait that ran out.
+constexpr unsigned kBadPage = 1, kBadLength = 2;
+
+// A batch as the kernels see it.
+struct Batch {
+    const int* table; int64_t table_stride;
+    const int* kv_len; const int* q_start;
+    int batch, max_pages, total_q, max_len, page_size, num_pages;
+    unsigned int* status;
+};
+
+// Sequence b's tokens in the cache, never more than its row of the page table holds.
+__device__ __forceinline__ int kv_length(const Batch& B, int b, bool report) {
+    const int n = B.kv_len[b];
+    const int64_t room = (int64_t)B.max_pages * B.page_size;
+    const int cap = room < B.max_len ? (int)room : B.max_len;
+    if (n >= 0 && n <= cap) return n;
+    if (report) atomicOr(B.status, kBadLength);
+    return n < 0 ? 0 : cap;
+}
+__device__ __forceinline__ int q_begin(const Batch& B, int b) { return min(max(B.q_start[b], 0), B.total_q); }
+
+struct Heads {
+    void* p; int64_t token_stride, head_stride; int heads;
+};
+inline Heads heads_of(const fd_heads& h) { return Heads{h.p_dev, h.token_stride, h.head_stride, h.heads}; }
+
+struct RowsArgs {                    // rotary positions, and an append when `append`
+    Heads x, y;                      // turned: x -> y (y may be x); heads 0: none
+    Heads k, v;                      // new rows of the cache (append)
+    void* k_pool; void* v_pool;
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+    const int* positions; const double* freqs;
+    Batch batch;
+    int tokens, head_dim, rot, layout, append;
+    float scale;                     // negative angles: sine times -1
+    float sign;
+};
+cudaError_t launch_rows(const RowsArgs& a, int dtype, int sm_count, cudaStream_t stream);
+
+struct EvictArgs {
+    Batch batch;
+    const float* w_in; float* w_out; int64_t w_stride;
+    const int* new_table; int64_t new_table_stride; int new_max_pages;
+    int keep, first, recent, heads, head_dim;
+    int* kept; int* new_len;
+    void* k_pool; void* v_pool;
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+};
+cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream);
+
+struct AttendArgs {
+    Batch batch;
+    Heads out;
+    int q_heads, heads, group, head_dim, dtype;
+    int tile_tokens;                 // tokens of a 128-row tile: 128 / group; its rows are (token, query head of the group)
+    int causal, window;              // window 0: none
+    float scale_log2;                // scale * log2(e)
+    float* lse;
+    const float* w_in; float* w_out; int64_t w_stride;
+    int splits, split_tiles;         // the cache in `splits` parts of split_tiles tiles of 128 tokens
+    float* part_o; float* part_lse;  // [split][token][query head]([head_dim])
+    int box_rows;
+    const void* v_pool; int64_t v_page, v_token, v_head;
+};
+// How many parts the cache is cut into, and the tiles of each.
+void attend_splits(int batch, int total_q, int max_len, int heads, int tile_tokens, int sm_count, int* splits, int* split_tiles);
+cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int sm_count, cudaStream_t stream);
+cudaError_t launch_weigh(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream);
+
+}  // namespace kv
+}  // namespace fd

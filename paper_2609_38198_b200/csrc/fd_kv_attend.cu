@@ -1,0 +1,736 @@
+// Attention of new tokens over a paged cache, and its column sums, on tcgen05 / TMEM.
+//
+// k_attend.  One CTA takes two tiles of 128 rows; a row is a (new token, query head of the group), so that all rows of a tile read the same cached
+// head.  Per tile of 128 cached tokens:
+//   S = Q K^T         (Q in shared memory, K by TMA page by page) into 128 fp32 columns of TMEM;
+//   m, P = 2^(c S - c m)   one thread a row: the maximum over the tile, then exponentials, rounded to the element type and written back over S.
+//                     The maximum in use is raised only when a row exceeds it by 2^8: sums and products stay exact in fp32 (P <= 2^8), and
+//                     the accumulator is read back and rescaled in the first tiles only;
+//   O += P V          (P in TMEM, V row-major in shared memory as an MN-major operand) into D fp32 columns.
+// While one tile's rows are exponentiated the tensor core works on the other's.  Rounding P to 16 bits changes a weight by half an ulp at
+// most, independently per weight; the norm sums the unrounded weights in fp32.
+//
+// Warps 0-3 / 4-7: softmax of row tile 0 / 1; 8: TMA; 9: MMA; 10, 11: values of tiles that some row sees only in part.  What a row does not see gets P = 0
+// exactly, but 0 x inf = NaN: in those tiles rows behind the sequence are zeroed in shared memory, and so are elements that are not finite; the latter
+// are added again at the end, row by row, to the rows that see them (never on finite data).
+// Every wait is bounded; on expiry the CTA raises a status word, lets its copies land, frees TMEM and exits.
+#include <algorithm>
+
+#include "fd_kv.h"
+#include "fd_tc_common.h"
+
+namespace fd {
+namespace kv {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreadsAt = 384;
+constexpr int kRegsLaunch = 168, kRegsSoft = 216, kRegsUtil = 72;
+static_assert(256 * kRegsSoft + 128 * kRegsUtil <= kThreadsAt * kRegsLaunch, "setmaxnreg must not ask for more than the launch has");
+constexpr float kLazy = 8.0f;            // the running maximum is raised when a score exceeds it by this many powers of two
+
+__device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ float max_nan(float a, float b) {       // a NaN is passed on
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+template <class T> struct Elem;
+template <> struct Elem<__nv_bfloat16> {
+    static constexpr uint32_t kFormat = 1, kExponent = 0x7f80u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ float at(const void* p, int64_t i) { return __bfloat162float(((const __nv_bfloat16*)p)[i]); }
+};
+template <> struct Elem<__half> {
+    static constexpr uint32_t kFormat = 0, kExponent = 0x7c00u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_f16x2(lo, hi); }
+    static __device__ __forceinline__ float at(const void* p, int64_t i) { return __half2float(((const __half*)p)[i]); }
+};
+// Instruction descriptor, fp32 accumulation, M = 128; `mn`: the B operand is MN-major.
+template <class T> constexpr uint32_t idesc_kv(int n, bool mn) {
+    return (1u << 4) | (Elem<T>::kFormat << 7) | (Elem<T>::kFormat << 10) | ((mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+template <int D>
+struct Geo {
+    static constexpr int kChunks = D / 64;                     // 128-byte columns of an operand tile
+    static constexpr int kChunkBytes = 128 * 128;              // 128 rows of one
+    static constexpr int kTile = kChunks * kChunkBytes;
+    static constexpr int kSlots = D == 128 ? 5 : 8;            // ring of key and value tiles
+    static constexpr int kSmem = 1024 + (2 + kSlots) * kTile + 512;
+    // Key and value tiles take turns in the ring; the j-th value tile is use number value_use(j) of its slot by values.
+    static __device__ __forceinline__ int value_use(int j) { return j / (kSlots % 2 ? kSlots : kSlots / 2); }
+};
+
+template <int D>
+struct Bars {
+    uint64_t q_full, full[Geo<D>::kSlots], empty[Geo<D>::kSlots], clean[Geo<D>::kSlots];
+    uint64_t s_full[2], p_full[2], pv_done[2];
+    uint32_t tmem_base;
+    int abort_flag, odd;                                        // odd: elements that are not finite were taken out of a tile
+};
+
+// Which rows a CTA works on: sequence, its first token, what it may see.
+struct Work {
+    int b, begin, count, n;           // sequence, its first row in q, its new tokens, its tokens in the cache
+    int t0;                           // first token of the first tile
+};
+// The slot-th group of `per` tokens of the batch, or b = -1.
+__device__ __forceinline__ Work find_work(const Batch& B, int slot, int per) {
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int b0 = 0; b0 < B.batch; b0 += 32) {
+        const int b = b0 + lane;
+        int begin = 0, count = 0;
+        if (b < B.batch) { begin = q_begin(B, b); count = max(0, q_begin(B, b + 1) - begin); }
+        const int tiles = (count + per - 1) / per;
+        int upto = tiles;
+        for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(~0u, upto, o); if (lane >= o) upto += v; }
+        const unsigned hit = __ballot_sync(~0u, slot < before + upto);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            Work w;
+            w.b = b0 + l;
+            w.begin = __shfl_sync(~0u, begin, l);
+            w.count = __shfl_sync(~0u, count, l);
+            w.t0 = (slot - before - __shfl_sync(~0u, upto - tiles, l)) * per;
+            w.n = kv_length(B, w.b, lane == 0);
+            return w;
+        }
+        before += __shfl_sync(~0u, upto, 31);
+    }
+    return Work{-1, 0, 0, 0, 0};
+}
+// Slots that token t of a sequence sees: [lo, hi).
+__device__ __forceinline__ int see_hi(const AttendArgs& a, const Work& w, int t) { return a.causal ? min(w.n, max(0, w.n - w.count + t + 1)) : w.n; }
+__device__ __forceinline__ int see_lo(const AttendArgs& a, const Work& w, int t) { return a.window ? max(0, w.n - w.count + t + 1 - a.window) : 0; }
+
+// Bits [lo, hi) of a 32-column group that begins at column c.
+__device__ __forceinline__ uint32_t col_mask(int lo, int hi, int c) {
+    const int l = min(max(lo - c, 0), 32), h = min(max(hi - c, 0), 32);
+    const uint32_t up = h >= 32 ? 0xffffffffu : (1u << h) - 1, down = l >= 32 ? 0xffffffffu : (1u << l) - 1;
+    return up & ~down;
+}
+
+// Loads 128 tokens of the cache from `tile` on into a ring slot; rows behind the sequence stay as they are.  One warp, converged.
+template <int D>
+__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, const AttendArgs& a, const Work& w, int tile, int h, uint64_t* bar) {
+    const int lane = threadIdx.x & 31, boxes = 128 / a.box_rows;
+    const int key = tile * 128 + lane * a.box_rows;
+    const bool mine = lane < boxes && key < w.n;
+    int page = 0;
+    if (mine) {
+        page = a.batch.table[w.b * a.batch.table_stride + key / a.batch.page_size];
+        if (page < 0 || page >= a.batch.num_pages) { page = a.batch.num_pages; atomicOr(a.batch.status, kBadPage); }   // (outside: TMA fills with zeros)
+    }
+    const int total = __popc(__ballot_sync(~0u, mine));
+    if (lane == 0) mbar_expect_tx(bar, total * a.box_rows * D * 2);
+    __syncwarp();
+    if (mine)
+#pragma unroll
+        for (int c = 0; c < Geo<D>::kChunks; ++c)
+            tma_load_4d(dst + c * Geo<D>::kChunkBytes + lane * a.box_rows * 128, map, c * 64, key % a.batch.page_size, h, page, bar);
+    __syncwarp();
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreadsAt, 1)
+k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+         const AttendArgs a) {
+    using G = Geo<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* base = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* q_base = base;
+    uint8_t* ring = base + 2 * G::kTile;
+    Bars<D>* bars = (Bars<D>*)(ring + G::kSlots * G::kTile);
+    volatile int* abort_flag = &bars->abort_flag;
+    unsigned int* status = a.batch.status + 1;
+
+    // work items: split fastest, then head, then token group, the last groups (which see most) first
+    const int split = blockIdx.x % a.splits, h = (blockIdx.x / a.splits) % a.heads;
+    const int groups = gridDim.x / (a.splits * a.heads), slot = groups - 1 - blockIdx.x / (a.splits * a.heads);
+    const int per = 2 * a.tile_tokens;
+    const Work w = find_work(a.batch, slot, per);
+    if (w.b < 0) return;
+    const int t_last = min(w.count, w.t0 + per) - 1;
+    const int tiles = (t_last - w.t0) / a.tile_tokens + 1;               // row tiles with work: 1 or 2
+    int j0 = see_lo(a, w, w.t0) / 128, j1 = (see_hi(a, w, t_last) + 127) / 128;
+    if (a.splits > 1) { j0 = max(j0, split * a.split_tiles); j1 = min(j1, (split + 1) * a.split_tiles); }
+    const int num = max(0, j1 - j0);
+    // tiles [full0, full1) are seen whole by every row
+    const int full0 = (see_lo(a, w, t_last) + 127) / 128, full1 = see_hi(a, w, w.t0) / 128;
+
+    const int warp = warp_index(), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        mbar_init(&bars->q_full, 1);
+        for (int s = 0; s < G::kSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); mbar_init(&bars->clean[s], 2); }
+        for (int t = 0; t < 2; ++t) { mbar_init(&bars->s_full[t], 1); mbar_init(&bars->p_full[t], 4); mbar_init(&bars->pv_done[t], 1); }
+        bars->abort_flag = 0; bars->odd = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUtil));
+        if (warp == 8 && num > 0) {
+            // ---------------------------------------------------------------- TMA
+            const int rows = a.tile_tokens * a.group;
+            if (lane == 0) {
+                mbar_expect_tx(&bars->q_full, tiles * rows * D * 2);
+                for (int t = 0; t < tiles; ++t)
+                    for (int c = 0; c < G::kChunks; ++c)
+                        tma_load_3d(q_base + t * G::kTile + c * G::kChunkBytes, &map_q, c * 64, h * a.group, w.begin + w.t0 + t * a.tile_tokens, &bars->q_full);
+            }
+            __syncwarp();
+            bool ok = true;
+            int it = 0;
+            for (; it < 2 * num; ++it) {
+                const int s = it % G::kSlots;
+                ok = mbar_wait(&bars->empty[s], ((it / G::kSlots) & 1) ^ 1, abort_flag, status, 1);
+                ok = __all_sync(~0u, ok);
+                if (!ok) break;
+                load_tile<D>(ring + s * G::kTile, (it & 1) ? &map_v : &map_k, a, w, j0 + it / 2, h, &bars->full[s]);
+            }
+            if (!ok && lane == 0) {             // aborted: copies in flight land before the CTA exits (bounded)
+                for (int k = max(0, it - G::kSlots); k < it; ++k) {
+                    const long long c0 = clock64();
+                    while (!mbar_try_wait(&bars->full[k % G::kSlots], (k / G::kSlots) & 1) && clock64() - c0 < 20000000ll) {}
+                }
+                const long long c0 = clock64();
+                while (!mbar_try_wait(&bars->q_full, 0) && clock64() - c0 < 20000000ll) {}
+            }
+        } else if (warp == 9 && num > 0) {
+            // ---------------------------------------------------------------- MMA (one thread)
+            if (elect_one()) {
+                constexpr uint32_t id_s = idesc_kv<T>(128, false), id_o = idesc_kv<T>(D, true);
+                const uint64_t qd = smem_desc(smem_u32(q_base), 1024, 2);
+                const uint64_t kd = smem_desc(smem_u32(ring), 1024, 2);
+                // values: rows of 64 coordinates are the MN direction (next 64: one chunk on), 8 tokens to the next 1024 bytes
+                const uint64_t vd = kd | ((uint64_t)(G::kChunkBytes >> 4) << 16);
+                const uint32_t q_lo = (uint32_t)qd, k_lo = (uint32_t)kd, v_lo = (uint32_t)vd, hi = (uint32_t)(kd >> 32);
+                auto scores = [&](int t, int slot_k) {
+                    const uint32_t s_addr = tmem + 128u * t, qt = q_lo + (uint32_t)(t * G::kTile >> 4), kt = k_lo + (uint32_t)(slot_k * G::kTile >> 4);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t o = (uint32_t)((k / 4) * (G::kChunkBytes >> 4) + (k % 4) * 2);
+                        if (k == 0) mma_ss2<0>(s_addr, qt + o, hi, kt + o, hi, id_s);
+                        else mma_ss2<1>(s_addr, qt + o, hi, kt + o, hi, id_s);
+                    }
+                    tc_commit(&bars->s_full[t]);
+                };
+                bool ok = mbar_wait(&bars->q_full, 0, abort_flag, status, 2) && mbar_wait(&bars->full[0], 0, abort_flag, status, 3);
+                if (ok) {
+                    tc_fence_after();
+                    for (int t = 0; t < tiles; ++t) scores(t, 0);
+                    tc_commit(&bars->empty[0]);
+                }
+                for (int j = 0; j < num && ok; ++j) {
+                    const int iv = 2 * j + 1, sv = iv % G::kSlots, ik = 2 * j + 2, sk = ik % G::kSlots;
+                    ok = mbar_wait(&bars->full[sv], (iv / G::kSlots) & 1, abort_flag, status, 4) &&
+                         mbar_wait(&bars->clean[sv], G::value_use(j) & 1, abort_flag, status, 5);
+                    for (int t = 0; t < tiles && ok; ++t) {
+                        ok = mbar_wait(&bars->p_full[t], j & 1, abort_flag, status, 6);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t o_addr = tmem + 256u + (uint32_t)D * t, p_addr = tmem + 128u * t, vt = v_lo + (uint32_t)(sv * G::kTile >> 4);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (k == 0 && j == 0) mma_ts2<0>(o_addr, p_addr, vt, hi, id_o);
+                            else mma_ts2<1>(o_addr, p_addr + 8 * k, vt + (uint32_t)(k * 2048 >> 4), hi, id_o);
+                        }
+                        tc_commit(&bars->pv_done[t]);
+                        if (j + 1 < num) {
+                            if (t == 0) {
+                                ok = mbar_wait(&bars->full[sk], (ik / G::kSlots) & 1, abort_flag, status, 7);
+                                if (!ok) break;
+                                tc_fence_after();
+                            }
+                            scores(t, sk);
+                        }
+                    }
+                    if (!ok) break;
+                    tc_commit(&bars->empty[sv]);
+                    if (j + 1 < num) tc_commit(&bars->empty[sk]);
+                }
+            }
+        } else if (warp >= 10 && num > 0) {
+            // ---------------------------------------------------------------- values that some row does not see
+            bool ok = true;
+            for (int j = 0; j < num; ++j) {
+                const int iv = 2 * j + 1, sv = iv % G::kSlots, tile = j0 + j;
+                ok = __all_sync(~0u, mbar_wait(&bars->full[sv], (iv / G::kSlots) & 1, abort_flag, status, 8));
+                if (!ok) break;
+                if (tile < full0 || tile >= full1) {
+                    uint8_t* v = ring + sv * G::kTile;
+                    bool odd = false;
+                    for (int i = threadIdx.x - 320; i < G::kTile / 16; i += 64) {       // 16 bytes of row (i / 8) % 128; the swizzle stays within the row
+                        uint4* p = (uint4*)(v + 16 * i);
+                        if (tile * 128 + (i / 8) % 128 >= w.n) { *p = make_uint4(0, 0, 0, 0); continue; }
+                        uint4 x = *p;
+                        uint32_t* e = &x.x;
+                        bool hit = false;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            constexpr uint32_t E = Elem<T>::kExponent;
+                            if ((e[k] & E) == E) { e[k] &= 0xffff0000u; hit = true; }
+                            if ((e[k] & (E << 16)) == (E << 16)) { e[k] &= 0xffffu; hit = true; }
+                        }
+                        if (hit) { *p = x; odd = true; }
+                    }
+                    if (odd) bars->odd = 1;
+                    fence_async();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->clean[sv]);
+            }
+        }
+    } else {
+        // -------------------------------------------------------------------- softmax (thread = row)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
+        const int t = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_addr = tmem + lane_addr + 128u * t, o_addr = tmem + lane_addr + 256u + (uint32_t)D * t;
+        const int token = w.t0 + t * a.tile_tokens + r / a.group, head = h * a.group + r % a.group;
+        const bool valid = r < a.tile_tokens * a.group && token < w.count;
+        const bool warp_on = __any_sync(~0u, valid);                     // warps without rows only keep the hand-offs going
+        const int lo = see_lo(a, w, token), hi = valid ? see_hi(a, w, token) : 0;
+        const float c = a.scale_log2;
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        if (t < tiles) {
+            for (int j = 0; j < num; ++j) {
+                const int tile = j0 + j;
+                ok = __all_sync(~0u, mbar_wait(&bars->s_full[t], j & 1, abort_flag, status, 9));
+                if (!ok) break;
+                if (warp_on) {
+                    tc_fence_after();
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) tmem_ld32(s_addr + 32 * k, s[k]);
+                    tmem_wait_ld();
+                    if (tile < full0 || tile >= full1) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t see = col_mask(lo, hi, tile * 128 + 32 * k);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!((see >> i) & 1)) s[k][i] = 0xff800000u;
+                        }
+                    }
+                    float mx[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        mx[k] = __uint_as_float(s[k][0]);
+#pragma unroll
+                        for (int i = 1; i < 32; ++i) mx[k] = max_nan(mx[k], __uint_as_float(s[k][i]));
+                    }
+                    const float top = max_nan(max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3])), m);
+                    const bool raise = !((top - m) * c <= kLazy) && top != m;        // (first tile: from -inf; a NaN goes through)
+                    if (__any_sync(~0u, raise)) {
+                        const float alpha = raise ? ex2f((m - top) * c) : 1.0f;
+                        if (raise) m = top;
+                        l *= alpha;
+                        if (j > 0) {
+                            if (!__all_sync(~0u, mbar_wait(&bars->pv_done[t], (j - 1) & 1, abort_flag, status, 10))) { ok = false; break; }
+                            tc_fence_after();
+#pragma unroll
+                            for (int k = 0; k < D / 32; ++k) {
+                                uint32_t o[32];
+                                tmem_ld32(o_addr + 32 * k, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st32(o_addr + 32 * k, o);
+                            }
+                        }
+                    }
+                    const float mc = m == -INFINITY ? 0.f : m * c;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t p[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float x0 = ex2f(fmaf(__uint_as_float(s[2 * k + i / 16][2 * (i % 16)]), c, -mc));
+                            const float x1 = ex2f(fmaf(__uint_as_float(s[2 * k + i / 16][2 * (i % 16) + 1]), c, -mc));
+                            sum[i & 1] += x0; sum[2 + (i & 1)] += x1;
+                            p[i] = Elem<T>::pack(x0, x1);
+                        }
+                        tmem_st32(s_addr + 32 * k, p);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_wait_st();
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->p_full[t]);
+            }
+            if (ok && num > 0) ok = __all_sync(~0u, mbar_wait(&bars->pv_done[t], (num - 1) & 1, abort_flag, status, 11));
+        }
+        if (ok && t < tiles && warp_on) {
+            tc_fence_after();
+            const bool empty = m == -INFINITY;
+            const float inv = empty ? 0.f : 1.0f / l;
+            const int64_t row = w.begin + token;
+            const bool odd = num > 0 && *(volatile int*)&bars->odd;
+            if (valid) {
+                if (a.splits > 1) a.part_lse[(split * (int64_t)a.batch.total_q + row) * a.q_heads + head] = empty ? -INFINITY : m * c + log2f(l);
+                else if (a.lse) a.lse[row * a.q_heads + head] = empty ? -INFINITY : (float)((double)(m * c + log2f(l)) * 0.69314718055994530942);
+            }
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                uint32_t u[32];
+                float o[32];
+                if (num > 0) { tmem_ld32(o_addr + 32 * k, u); tmem_wait_ld(); }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = empty ? 0.f : __uint_as_float(u[i]) * inv;
+                if (odd && valid) {
+                    // what is not finite in tiles that this CTA's rows see in part, for the rows that see it
+                    for (int key = max(lo, j0 * 128); key < min(hi, j1 * 128); ++key) {
+                        if (key / 128 >= full0 && key / 128 < full1) { key = full1 * 128 - 1; continue; }
+                        const int page = a.batch.table[w.b * a.batch.table_stride + key / a.batch.page_size];
+                        if (page < 0 || page >= a.batch.num_pages) continue;
+                        const int64_t at = page * a.v_page + (key % a.batch.page_size) * a.v_token + h * a.v_head + 32 * k;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float v = Elem<T>::at(a.v_pool, at + i);
+                            if (!isfinite(v)) o[i] += v;
+                        }
+                    }
+                }
+                if (valid) {
+                    if (a.splits > 1) {
+                        float4* dst = (float4*)(a.part_o + ((split * (int64_t)a.batch.total_q + row) * a.q_heads + head) * D + 32 * k);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    } else {
+                        uint4* dst = (uint4*)((T*)a.out.p + row * a.out.token_stride + head * a.out.head_stride + 32 * k);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            dst[i] = make_uint4(Elem<T>::pack(o[8 * i], o[8 * i + 1]), Elem<T>::pack(o[8 * i + 2], o[8 * i + 3]),
+                                                Elem<T>::pack(o[8 * i + 4], o[8 * i + 5]), Elem<T>::pack(o[8 * i + 6], o[8 * i + 7]));
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+// Joins the parts of the cache: out = sum_s 2^(lse_s - lse) o_s.  One warp a row.
+template <class T, int D>
+__global__ void __launch_bounds__(256) k_join(const AttendArgs a) {
+    grid_wait();
+    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    const int64_t rows = (int64_t)q_begin(a.batch, a.batch.batch) * a.q_heads, all = (int64_t)a.batch.total_q * a.q_heads;
+    if (row >= rows) return;
+    float top = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) top = max_nan(top, a.part_lse[s * all + row]);
+    constexpr int E = D / 32;
+    float o[E], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] = 0.f;
+    for (int s = 0; s < a.splits && top != -INFINITY; ++s) {
+        const float part = a.part_lse[s * all + row];
+        if (part == -INFINITY) continue;                       // (its o was not written)
+        const float f = ex2f(part - top);
+        const float* p = a.part_o + (s * all + row) * D + lane * E;
+        sum += f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] = fmaf(f, p[i], o[i]);
+    }
+    const float inv = top == -INFINITY ? 0.f : 1.0f / sum;
+    const int64_t token = row / a.q_heads;
+    const int head = (int)(row - token * a.q_heads);
+    uint32_t* dst = (uint32_t*)((T*)a.out.p + token * a.out.token_stride + head * a.out.head_stride + lane * E);
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) dst[i] = Elem<T>::pack(o[2 * i] * inv, o[2 * i + 1] * inv);
+    if (a.lse && lane == 0) a.lse[row] = top == -INFINITY ? -INFINITY : (float)((double)(top + log2f(sum)) * 0.69314718055994530942);
+}
+
+// k_weigh: what every cached token received, w_j += sum over rows of 2^(c s - lse).  One CTA takes two tiles of 128 cached tokens as the M side (S^T = K Q^T: a
+// thread owns a token, so the sum over rows is a sum over its columns and needs no exchange) and goes through the rows that see them.
+constexpr int kWeighSlots = 3;
+template <int D>
+struct WeighSmem {
+    static constexpr int kBytes = 1024 + (2 + kWeighSlots) * Geo<D>::kTile + 4 * 128 * 4 + 512;
+};
+struct WeighBars {
+    uint64_t k_full, full[kWeighSlots], empty[kWeighSlots], s_full[2][2], s_empty[2][2], l_full[4];
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreadsAt, 1)
+k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const AttendArgs a) {
+    using G = Geo<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* base = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* k_base = base;
+    uint8_t* ring = base + 2 * G::kTile;
+    float* l_ring = (float*)(ring + kWeighSlots * G::kTile);                  // [4][128]: -lse of a row tile, -inf for rows that are none
+    WeighBars* bars = (WeighBars*)(l_ring + 4 * 128);
+    volatile int* abort_flag = &bars->abort_flag;
+    unsigned int* status = a.batch.status + 1;
+
+    const int h = blockIdx.y, b = blockIdx.z, key0 = blockIdx.x * 256;
+    Work w;
+    w.b = b; w.begin = q_begin(a.batch, b); w.count = max(0, q_begin(a.batch, b + 1) - w.begin); w.n = kv_length(a.batch, b, false); w.t0 = 0;
+    if (key0 >= w.n) return;
+    const int tiles = w.n - key0 > 128 ? 2 : 1, key_last = min(w.n, key0 + 256) - 1, off = w.n - w.count;
+    // tokens that see one of these slots: [ta, tb)
+    const int ta = a.causal ? max(0, key0 - off) : 0, tb = a.window ? min((int64_t)w.count, max((int64_t)0, (int64_t)key_last - off + a.window)) : w.count;
+    const int q0 = ta / a.tile_tokens, num = tb > ta ? (tb - 1) / a.tile_tokens + 1 - q0 : 0;
+    const int rows = a.tile_tokens * a.group;
+
+    const int warp = warp_index(), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        mbar_init(&bars->k_full, 1);
+        for (int s = 0; s < kWeighSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&bars->s_full[i >> 1][i & 1], 1); mbar_init(&bars->s_empty[i >> 1][i & 1], 4); mbar_init(&bars->l_full[i], 1); }
+        bars->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;
+
+    if (warp == 8 && num > 0) {
+        // -------------------------------------------------------------------- TMA
+        bool ok = true;
+        {   // both key tiles arrive on one barrier: bytes first, then the copies
+            const int boxes = 128 / a.box_rows;
+            int count = 0;
+            for (int t = 0; t < tiles; ++t) count += __popc(__ballot_sync(~0u, lane < boxes && key0 + t * 128 + lane * a.box_rows < w.n));
+            if (lane == 0) mbar_expect_tx(&bars->k_full, count * a.box_rows * D * 2);
+            __syncwarp();
+            for (int t = 0; t < tiles; ++t) {
+                const int key = key0 + t * 128 + lane * a.box_rows;
+                if (lane < boxes && key < w.n) {
+                    int page = a.batch.table[b * a.batch.table_stride + key / a.batch.page_size];
+                    if (page < 0 || page >= a.batch.num_pages) { page = a.batch.num_pages; atomicOr(a.batch.status, kBadPage); }
+#pragma unroll
+                    for (int c = 0; c < G::kChunks; ++c)
+                        tma_load_4d(k_base + t * G::kTile + c * G::kChunkBytes + lane * a.box_rows * 128, &map_k, c * 64, key % a.batch.page_size, h, page, &bars->k_full);
+                }
+            }
+            __syncwarp();
+        }
+        int it = 0;
+        if (lane == 0) {
+            for (; it < num && ok; ++it) {
+                const int s = it % kWeighSlots;
+                ok = mbar_wait(&bars->empty[s], ((it / kWeighSlots) & 1) ^ 1, abort_flag, status, 21);
+                if (!ok) break;
+                mbar_expect_tx(&bars->full[s], rows * D * 2);
+                for (int c = 0; c < G::kChunks; ++c)
+                    tma_load_3d(ring + s * G::kTile + c * G::kChunkBytes, &map_q, c * 64, h * a.group, w.begin + (q0 + it) * a.tile_tokens, &bars->full[s]);
+            }
+            if (!ok) {
+                for (int k = max(0, it - kWeighSlots); k < it; ++k) {
+                    const long long c0 = clock64();
+                    while (!mbar_try_wait(&bars->full[k % kWeighSlots], (k / kWeighSlots) & 1) && clock64() - c0 < 20000000ll) {}
+                }
+                const long long c0 = clock64();
+                while (!mbar_try_wait(&bars->k_full, 0) && clock64() - c0 < 20000000ll) {}
+            }
+        }
+    } else if (warp == 9 && num > 0) {
+        // -------------------------------------------------------------------- MMA (one thread)
+        if (elect_one()) {
+            constexpr uint32_t id = idesc_kv<T>(128, false);
+            const uint64_t kd = smem_desc(smem_u32(k_base), 1024, 2), qd = smem_desc(smem_u32(ring), 1024, 2);
+            const uint32_t k_lo = (uint32_t)kd, q_lo = (uint32_t)qd, hi = (uint32_t)(kd >> 32);
+            bool ok = mbar_wait(&bars->k_full, 0, abort_flag, status, 22);
+            for (int i = 0; i < num && ok; ++i) {
+                const int s = i % kWeighSlots, buf = i & 1;
+                ok = mbar_wait(&bars->full[s], (i / kWeighSlots) & 1, abort_flag, status, 23);
+                for (int t = 0; t < tiles && ok; ++t) {
+                    ok = mbar_wait(&bars->s_empty[t][buf], ((i >> 1) & 1) ^ 1, abort_flag, status, 24);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t s_addr = tmem + 256u * t + 128u * buf, kt = k_lo + (uint32_t)(t * G::kTile >> 4), qt = q_lo + (uint32_t)(s * G::kTile >> 4);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t o = (uint32_t)((k / 4) * (G::kChunkBytes >> 4) + (k % 4) * 2);
+                        if (k == 0) mma_ss2<0>(s_addr, kt + o, hi, qt + o, hi, id);
+                        else mma_ss2<1>(s_addr, kt + o, hi, qt + o, hi, id);
+                    }
+                    tc_commit(&bars->s_full[t][buf]);
+                }
+                if (ok) tc_commit(&bars->empty[s]);
+            }
+        }
+    } else if (warp == 10 && num > 0) {
+        // -------------------------------------------------------------------- -lse of each row tile, in powers of two
+        bool ok = true;
+        for (int i = 0; i < num; ++i) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = lane + 32 * k, token = (q0 + i) * a.tile_tokens + r / a.group;
+                v[k] = -INFINITY;
+                if (r < rows && token < w.count) {
+                    const float lse = a.lse[(int64_t)(w.begin + token) * a.q_heads + h * a.group + r % a.group];
+                    if (lse != -INFINITY) v[k] = (float)((double)lse * -1.44269504088896340736);
+                }
+            }
+            // slot i % 4 may be written once tile i - 4 has been read; waiting for tile i - 2, whose buffer hand-back is the latest that can have happened, is enough
+            if (i >= 2)
+                for (int t = 0; t < tiles && ok; ++t) ok = mbar_wait(&bars->s_empty[t][i & 1], ((i >> 1) & 1) ^ 1, abort_flag, status, 25);
+            ok = __all_sync(~0u, ok);
+            if (!ok) break;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) l_ring[(i & 3) * 128 + lane + 32 * k] = v[k];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->l_full[i & 3]);
+        }
+    } else if (warp < 8) {
+        const int t = warp >> 2, key = key0 + t * 128 + (warp & 3) * 32 + lane;
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        float acc0 = 0.f, acc1 = 0.f;
+        bool ok = true;
+        if (t < tiles) {
+            for (int i = 0; i < num; ++i) {
+                const int buf = i & 1, tok0 = (q0 + i) * a.tile_tokens;
+                ok = __all_sync(~0u, mbar_wait(&bars->l_full[i & 3], (i >> 2) & 1, abort_flag, status, 26) &&
+                                     mbar_wait(&bars->s_full[t][buf], (i >> 1) & 1, abort_flag, status, 27));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t addr = tmem + lane_addr + 256u * t + 128u * buf;
+                const float* lr = l_ring + (i & 3) * 128;
+                // columns of rows that see this token: [cl, ch)
+                const int valid = min(rows, (w.count - tok0) * a.group);
+                int cl = 0, ch = valid;
+                if (a.causal) cl = max(0, key - off - tok0) * a.group;
+                if (a.window) ch = (int)min((int64_t)valid, max((int64_t)0, (int64_t)key - off + a.window - tok0) * a.group);
+                const bool whole = __all_sync(~0u, cl == 0 && ch >= 128);
+                for (int k = 0; k < 4 && 32 * k < valid; ++k) {
+                    uint32_t s[32];
+                    tmem_ld32(addr + 32 * k, s);
+                    tmem_wait_ld();
+                    const uint32_t see = whole ? 0xffffffffu : col_mask(cl, ch, 32 * k);
+                    float p[32];
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) p[x] = ex2f(fmaf(__uint_as_float(s[x]), a.scale_log2, lr[32 * k + x]));
+                    if (!whole)
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) if (!((see >> x) & 1)) p[x] = 0.f;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) sum[x & 3] += p[x];
+                    acc0 += sum[0] + sum[1];
+                    acc1 += sum[2] + sum[3];
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->s_empty[t][buf]);
+            }
+            if (ok && key < w.n) {
+                const int64_t at = ((int64_t)b * a.heads + h) * a.w_stride + key;
+                a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + (acc0 + acc1);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+template <class T, int D>
+cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
+    cudaError_t e = cudaFuncSetAttribute(k_attend<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<D>::kSmem);
+    if (e != cudaSuccess) return e;
+    cudaFuncAttributes fa;
+    if ((e = cudaFuncGetAttributes(&fa, k_attend<T, D>)) != cudaSuccess) return e;
+    if (fa.numRegs != kRegsLaunch) return cudaErrorInvalidKernelImage;             // the split of the registers counts on it
+    const int64_t groups = a.batch.total_q / (2 * a.tile_tokens) + std::min(a.batch.batch, a.batch.total_q);
+    k_attend<T, D><<<(unsigned)(groups * a.heads * a.splits), kThreadsAt, Geo<D>::kSmem, stream>>>(mq, mk, mv, a);
+    ++g_launches;
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (a.splits > 1) {
+        ++g_launches;
+        e = launch_behind(stream, dim3((unsigned)ceil_div((int64_t)a.batch.total_q * a.q_heads, 8)), dim3(256), 0, k_join<T, D>, a);
+    }
+    return e;
+}
+template <class T, int D>
+cudaError_t weigh_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
+    cudaError_t e = cudaFuncSetAttribute(k_weigh<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeighSmem<D>::kBytes);
+    if (e != cudaSuccess) return e;
+    k_weigh<T, D><<<dim3((unsigned)ceil_div(a.batch.max_len, 256), a.heads, a.batch.batch), kThreadsAt, WeighSmem<D>::kBytes, stream>>>(mq, mk, a);
+    ++g_launches;
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+void attend_splits(int batch, int total_q, int max_len, int heads, int tile_tokens, int sm_count, int* splits, int* split_tiles) {
+    // parts of at least two tiles, as many as fill the GPU once if every sequence were as long as the longest
+    const int64_t ctas = ((int64_t)total_q / (2 * tile_tokens) + std::min(batch, total_q)) * heads, tiles = ceil_div(max_len, 128);
+    int64_t s = ctas >= sm_count ? 1 : sm_count / std::max<int64_t>(ctas, 1);
+    s = std::max<int64_t>(1, std::min<int64_t>(s, tiles / 2));
+    const int64_t per = std::max<int64_t>(1, ceil_div(tiles, s));
+    *split_tiles = (int)per;
+    *splits = (int)std::max<int64_t>(1, ceil_div(tiles, per));
+}
+
+#define FD_KV_PICK(fn, ...)                                                                                     \
+    (a.dtype == FD_BF16 ? (a.head_dim == 128 ? fn<__nv_bfloat16, 128>(__VA_ARGS__) : fn<__nv_bfloat16, 64>(__VA_ARGS__)) \
+                        : (a.head_dim == 128 ? fn<__half, 128>(__VA_ARGS__) : fn<__half, 64>(__VA_ARGS__)))
+
+cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int, cudaStream_t stream) {
+    return FD_KV_PICK(attend_t, a, mq, mk, mv, stream);
+}
+cudaError_t launch_weigh(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
+    return FD_KV_PICK(weigh_t, a, mq, mk, stream);
+}
+
+}  // namespace kv
+}  // namespace fd
