@@ -439,7 +439,8 @@ typedef struct {
     float*   lse_dev;
     const float* weights_in_dev; float* weights_out_dev; int64_t weights_stride;
 } fd_kv_attend_args;
-size_t    fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* batch, int32_t q_heads);
+/* Workspace of a call, with `weights` of one that has weights_out; 0: none is needed (or the arguments are wrong). */
+size_t    fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* batch, int32_t q_heads, int32_t weights);
 fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_attend_args* args, void* workspace_dev,
                        size_t workspace_bytes, void* cuda_stream, char* errbuf, size_t errbuf_len);
 

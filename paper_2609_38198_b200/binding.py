@@ -140,7 +140,7 @@ def _load() -> ctypes.CDLL:
     lib.fd_kv_destroy.restype = None
     lib.fd_kv_synchronize.argtypes = [c_void_p, c_void_p]
     lib.fd_kv_append.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_append_args), c_void_p, c_char_p, c_size_t]
-    lib.fd_kv_attend_bytes.argtypes = [c_void_p, POINTER(fd_kv_batch), c_int32]
+    lib.fd_kv_attend_bytes.argtypes = [c_void_p, POINTER(fd_kv_batch), c_int32, c_int32]
     lib.fd_kv_attend_bytes.restype = c_size_t
     lib.fd_kv_attend.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_attend_args), c_void_p, c_size_t, c_void_p, c_char_p, c_size_t]
     lib.fd_kv_evict.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_evict_args), c_void_p, c_char_p, c_size_t]
@@ -425,30 +425,43 @@ _LAYOUTS = {"half": FD_ROTARY_HALF, "interleaved": FD_ROTARY_INTERLEAVED}
 _SCALINGS = {"none": FD_ROTARY_PLAIN, "linear": FD_ROTARY_LINEAR, "base": FD_ROTARY_BASE, "ramp": FD_ROTARY_RAMP}
 
 
+def _refuse(what: str):
+    raise FdError(FD_ERR_INVALID, what)
+
+
 def _need(cond, what: str):
     if not cond:
-        raise FdError(FD_ERR_INVALID, what)
+        _refuse(what)
 
 
+# (These checks and the calls below run once per operator and decoding step, some in less time than the kernel they launch: texts are made where a check fails.)
 def _need_tensor(t, dtype, dims: int, device, what: str):
-    _need(isinstance(t, torch.Tensor) and t.dtype == dtype and t.dim() == dims and t.device == device, f"{what}: a {dims}-d {dtype} tensor on {device}")
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != dims or t.device != device:
+        _refuse(f"{what}: a {dims}-d {dtype} tensor on {device}")
 
 
 def _heads(t: torch.Tensor, dtype, device, head_dim: int, tokens: int, what: str) -> fd_heads:
     """[tokens, heads, head_dim] with unit stride inside a head; strides of single tokens and heads do not matter."""
-    _need_tensor(t, dtype, 3, device, what)
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 3 or t.device != device:
+        _refuse(f"{what}: a 3-d {dtype} tensor on {device}")
     n, h, d = t.shape
     st, sh, sd = t.stride()
-    _need(n == tokens and d == head_dim and (sd == 1 or d == 1), f"{what}: [{tokens}, heads, {head_dim}] with unit stride inside a head")
+    if n != tokens or d != head_dim or (sd != 1 and d != 1):
+        _refuse(f"{what}: [{tokens}, heads, {head_dim}] with unit stride inside a head")
     return fd_heads(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d, h)
 
 
-def _stream(device) -> c_void_p:
-    return c_void_p(torch.cuda.current_stream(device).cuda_stream)
-
-
-def _raise(st: int, err):
-    raise FdError(st, err.value.decode())
+def _call(device, fn, *args):
+    """fn(*args, current stream, errbuf, its length) on `device`.  An argument error leaves no launch behind, so the call is made without a buffer for
+    the message and repeated with one when it was refused."""
+    with _on(device):
+        stream = torch._C._cuda_getCurrentRawStream(device.index)
+        st = fn(*args, stream, None, 0)
+        if st != FD_OK:
+            err = ctypes.create_string_buffer(256)
+            if st in (FD_ERR_INVALID, FD_ERR_WORKSPACE, FD_ERR_UNSUPPORTED):
+                fn(*args, stream, err, 256)
+            raise FdError(st, err.value.decode())
 
 
 def fd_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -465,10 +478,11 @@ def fd_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "n
 def _rotary_args(positions, freqs, tokens: int, device, layout: str):
     _need_tensor(positions, torch.int32, 1, device, "positions")
     _need_tensor(freqs, torch.float64, 1, device, "freqs")
-    _need(positions.shape[0] == tokens and positions.is_contiguous(), f"positions: {tokens} contiguous values")
+    if positions.shape[0] != tokens or not positions.is_contiguous():
+        _refuse(f"positions: {tokens} contiguous values")
     _need(freqs.is_contiguous(), "freqs must be contiguous")
-    _need(layout in _LAYOUTS, f"layout: one of {sorted(_LAYOUTS)}")
-    return _LAYOUTS[layout]
+    code = _LAYOUTS.get(layout)
+    return code if code is not None else _refuse(f"layout: one of {sorted(_LAYOUTS)}")
 
 
 def fd_rotary(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, layout: str = "half", scale: float = 1.0,
@@ -478,14 +492,10 @@ def fd_rotary(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, lay
     _need(isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 3 and x.dtype in _DTYPES, "x: a CUDA tensor [tokens, heads, head_dim] of bf16, fp16 or fp32")
     tokens, _, d = x.shape
     code = _rotary_args(positions, freqs, tokens, x.device, layout)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
     hx, hy = _heads(x, x.dtype, x.device, d, tokens, "x"), _heads(y, x.dtype, x.device, d, tokens, "out")
-    err = ctypes.create_string_buffer(256)
-    with _on(x.device):
-        st = lib.fd_rotary(byref(hx), byref(hy), _DTYPES[x.dtype], tokens, d, positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0],
-                           code, scale, 1 if inverse else 0, _stream(x.device), err, 256)
-    if st != FD_OK:
-        _raise(st, err)
+    _call(x.device, lib.fd_rotary, byref(hx), byref(hy), _DTYPES[x.dtype], tokens, d, positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0],
+          code, scale, 1 if inverse else 0)
     return y
 
 
@@ -509,6 +519,7 @@ class KVBatch:
         self.batch, self.max_len = n, int(max_len)
         self.struct = fd_kv_batch(page_table.data_ptr(), max(page_table.stride(0), page_table.shape[1]), kv_len.data_ptr(), q_start.data_ptr(), n,
                                   page_table.shape[1], total_q, max_new, max_len)
+        self.ref = byref(self.struct)
 
 
 class KVCache:
@@ -535,7 +546,7 @@ class KVCache:
             torch.cuda.current_stream(dev).synchronize()       # the status words are zero for every stream from here on
             st = lib.fd_kv_create(byref(h), byref(desc), err, 256)
         if st != FD_OK:
-            _raise(st, err)
+            raise FdError(st, err.value.decode())
         self._h = h
 
     def close(self):
@@ -552,13 +563,14 @@ class KVCache:
     def synchronize(self):
         """Waits for the current stream; raises FdError if a page number or length was out of range, or a bounded wait ran out."""
         with _on(self.device):
-            st = lib.fd_kv_synchronize(self._h, _stream(self.device))
+            st = lib.fd_kv_synchronize(self._h, torch._C._cuda_getCurrentRawStream(self.device.index))
         if st != FD_OK:
             raise FdError(st, "a page number or a length was out of range" if st == FD_ERR_INVALID else "")
 
     def _batch(self, batch: KVBatch):
-        _need(batch.device == self.device, f"the batch is on {batch.device}, the cache on {self.device}")
-        return byref(batch.struct)
+        if batch.device != self.device:
+            _refuse(f"the batch is on {batch.device}, the cache on {self.device}")
+        return batch.ref
 
     def append(self, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor | None = None, freqs: torch.Tensor | None = None,
                layout: str = "half", scale: float = 1.0, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
@@ -571,13 +583,9 @@ class KVCache:
         a.scale = scale
         if q is not None:
             a.q = _heads(q, dt, dev, d, n, "q")
-            q_out = torch.empty(q.shape, dtype=dt, device=dev) if q_out is None else q_out
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
             a.q_out = _heads(q_out, dt, dev, d, n, "q_out")
-        err = ctypes.create_string_buffer(256)
-        with _on(dev):
-            st = lib.fd_kv_append(self._h, self._batch(batch), byref(a), _stream(dev), err, 256)
-        if st != FD_OK:
-            _raise(st, err)
+        _call(dev, lib.fd_kv_append, self._h, self._batch(batch), byref(a))
         return q_out
 
     def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, causal: bool = True, window: int = 0,
@@ -589,11 +597,12 @@ class KVCache:
         n, dev, dt, d = batch.total_q, self.device, self.dtype, self.head_dim
         hq = _heads(q, dt, dev, d, n, "q")
         if out is None:
-            out = torch.empty(q.shape, dtype=dt, device=dev)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if lse is None:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
-        _need_tensor(lse, torch.float32, 2, dev, "lse")
-        _need(lse.shape == q.shape[:2] and lse.is_contiguous(), "lse: [total_q, query heads], contiguous")
+            lse = torch.empty((n, hq.heads), dtype=torch.float32, device=dev)
+        else:
+            _need_tensor(lse, torch.float32, 2, dev, "lse")
+            _need(lse.shape == q.shape[:2] and lse.is_contiguous(), "lse: [total_q, query heads], contiguous")
         a = fd_kv_attend_args(hq, _heads(out, dt, dev, d, n, "out"), d ** -0.5 if scale is None else scale, 1 if causal else 0, window or 0, lse.data_ptr())
         if weights is not None or weights_out is not None:
             weights_out = weights if weights_out is None else weights_out
@@ -603,19 +612,17 @@ class KVCache:
                     _need(t.stride() == weights_out.stride(), "weights and weights_out: equal strides")
             a.weights_in_dev, a.weights_out_dev = _ptr(weights), weights_out.data_ptr()
             a.weights_stride = weights_out.stride(1)
-        b, err = self._batch(batch), ctypes.create_string_buffer(256)
-        with _on(dev):
-            size = lib.fd_kv_attend_bytes(self._h, b, hq.heads)
-            ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
-            st = lib.fd_kv_attend(self._h, b, byref(a), _ptr(ws), size, _stream(dev), err, 256)
-        if st != FD_OK:
-            _raise(st, err)
+        b = self._batch(batch)
+        size = lib.fd_kv_attend_bytes(self._h, b, hq.heads, 1 if weights_out is not None else 0)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+        _call(dev, lib.fd_kv_attend, self._h, b, byref(a), _ptr(ws), size)
         return out, lse
 
     def _check_weights(self, t: torch.Tensor, batch: KVBatch):
         _need_tensor(t, torch.float32, 3, self.device, "weights")
-        _need(t.shape[0] == batch.batch and t.shape[1] == self.heads and t.shape[2] >= batch.max_len and t.is_contiguous(),
-              f"weights: [{batch.batch}, {self.heads}, {batch.max_len} or more], contiguous")
+        n, h, length = t.shape
+        if n != batch.batch or h != self.heads or length < batch.max_len or not t.is_contiguous():
+            _refuse(f"weights: [{batch.batch}, {self.heads}, {batch.max_len} or more], contiguous")
 
     def evict(self, batch: KVBatch, weights: torch.Tensor, keep: int, first: int = 0, recent: int = 0, new_table: torch.Tensor | None = None,
               kept: torch.Tensor | None = None, new_len: torch.Tensor | None = None, weights_out: torch.Tensor | None = None):
@@ -635,15 +642,13 @@ class KVCache:
             new_len = torch.empty(batch.batch, dtype=torch.int32, device=dev)
         _need_tensor(kept, torch.int32, 3, dev, "kept")
         _need_tensor(new_len, torch.int32, 1, dev, "new_len")
-        _need(tuple(kept.shape) == (batch.batch, self.heads, keep) and kept.is_contiguous(), f"kept: [{batch.batch}, {self.heads}, {keep}], contiguous")
-        _need(new_len.shape[0] == batch.batch and new_len.is_contiguous(), f"new_len: {batch.batch} contiguous values")
+        if kept.shape != (batch.batch, self.heads, keep) or not kept.is_contiguous():
+            _refuse(f"kept: [{batch.batch}, {self.heads}, {keep}], contiguous")
+        if new_len.shape[0] != batch.batch or not new_len.is_contiguous():
+            _refuse(f"new_len: {batch.batch} contiguous values")
         a = fd_kv_evict_args(weights.data_ptr(), weights_out.data_ptr(), weights.stride(1), table.data_ptr(), max(table.stride(0), table.shape[1]),
                              table.shape[1], keep, first, recent, kept.data_ptr(), new_len.data_ptr())
-        err = ctypes.create_string_buffer(256)
-        with _on(dev):
-            st = lib.fd_kv_evict(self._h, self._batch(batch), byref(a), _stream(dev), err, 256)
-        if st != FD_OK:
-            _raise(st, err)
+        _call(dev, lib.fd_kv_evict, self._h, self._batch(batch), byref(a))
         return kept, new_len, weights_out
 
 

@@ -2,7 +2,7 @@
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
-#include <limits>
+#include <algorithm>
 #include <new>
 
 #include "fd_kv.h"
@@ -81,7 +81,7 @@ fd_status check_batch(const Err& err, const fd_kv* kv, const fd_kv_batch* b, boo
     if (b->batch == 0) return FD_OK;
     if (!b->table_dev || !b->kv_len_dev || (queries && !b->q_start_dev)) return err(FD_ERR_INVALID, "page table, lengths and starts must be non-null");
     if (b->max_pages < 1 || b->table_stride < b->max_pages) return err(FD_ERR_INVALID, "bad page table: %d pages a row, stride %lld", b->max_pages, (long long)b->table_stride);
-    if (b->total_q < 0 || b->max_new < 0 || b->max_new > b->total_q || b->max_len < 0) return err(FD_ERR_INVALID, "bad bounds: total_q %d, max_new %d, max_len %d", b->total_q, b->max_new, b->max_len);
+    if (b->total_q < 0 || b->max_new < 0 || b->max_new > b->total_q || (b->max_new == 0 && b->total_q > 0) || b->max_len < 0) return err(FD_ERR_INVALID, "bad bounds: total_q %d, max_new %d, max_len %d", b->total_q, b->max_new, b->max_len);
     if (b->max_len > (1 << 30) || b->total_q > (1 << 30)) return err(FD_ERR_UNSUPPORTED, "lengths up to 2^30 tokens are covered");
     return FD_OK;
 }
@@ -107,6 +107,32 @@ bool overlap(const fd_heads& a, const fd_heads& b, int tokens, int head_dim, int
 bool same(const fd_heads& a, const fd_heads& b) { return a.p_dev == b.p_dev && a.token_stride == b.token_stride && a.head_stride == b.head_stride && a.heads == b.heads; }
 
 }  // namespace
+
+// Few rows a sequence: one row tile of 16, bound by the cache's bytes.  The cache is cut into parts of 256 tokens or more until four rounds of CTAs (two fit an
+// SM) run, so that uneven lengths even out.  Else: parts of at least two tiles of 128, as many as fill the GPU once if every sequence were as long as the longest.
+Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weights) {
+    Plan p{};
+    const int64_t heads = kv->d.heads, group = q_heads / heads, sms = kv->sm_count, live = std::min(b->batch, b->total_q);
+    p.few = (int64_t)b->max_new * group <= kFewRows;
+    const int64_t unit = p.few ? 64 : 128, tiles = std::max<int64_t>(1, ceil_div(b->max_len, unit));
+    int64_t s;
+    if (p.few) {
+        s = std::max<int64_t>(1, std::min(ceil_div(8 * sms, live * heads), tiles / 4));
+    } else {
+        const int64_t ctas = (b->total_q / (2 * (128 / group)) + live) * heads;
+        s = std::max<int64_t>(1, std::min(sms / ctas, tiles / 2));
+    }
+    p.split_tiles = (int)ceil_div(tiles, s);
+    p.splits = (int)ceil_div(tiles, p.split_tiles);
+    const size_t rows = (size_t)b->total_q * q_heads;
+    if (p.splits > 1) { p.part_o = (size_t)p.splits * rows * kv->d.head_dim; p.part_lse = (size_t)p.splits * rows; }
+    if (p.few && weights) {
+        p.score_stride = round_up(b->max_len, 64);
+        p.scores = (size_t)b->batch * heads * kFewRows * p.score_stride;
+    }
+    return p;
+}
+
 }  // namespace kv
 }  // namespace fd
 
@@ -187,8 +213,10 @@ fd_status fd_kv_create(fd_kv** out, const fd_kv_desc* d, char* errbuf, size_t er
     if (e != cudaSuccess) { delete kv; return err.cuda(e, "device"); }
     const uint64_t dims[4] = {(uint64_t)d->head_dim, (uint64_t)d->page_size, (uint64_t)d->heads, (uint64_t)d->num_pages};
     const uint32_t box[4] = {64, (uint32_t)kv->box_rows, 1, 1};
+    const uint32_t few[4] = {64, (uint32_t)(kv->few_rows = g < 16 ? g : 16), 1, 1};
     const int64_t ks[3] = {d->k_token_stride, d->k_head_stride, d->k_page_stride}, vs[3] = {d->v_token_stride, d->v_head_stride, d->v_page_stride};
-    if (!make_map(&kv->map_k, d->k_dev, d->dtype, 4, dims, ks, box) || !make_map(&kv->map_v, d->v_dev, d->dtype, 4, dims, vs, box)) {
+    if (!make_map(&kv->map_k, d->k_dev, d->dtype, 4, dims, ks, box) || !make_map(&kv->map_v, d->v_dev, d->dtype, 4, dims, vs, box) ||
+        !make_map(&kv->few_k, d->k_dev, d->dtype, 4, dims, ks, few) || !make_map(&kv->few_v, d->v_dev, d->dtype, 4, dims, vs, few)) {
         delete kv;
         return err(FD_ERR_CUDA, "cuTensorMapEncodeTiled refused the pools");
     }
@@ -245,11 +273,10 @@ fd_status fd_kv_append(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_append
     return e == cudaSuccess ? FD_OK : err.cuda(e, "k_rows");
 }
 
-size_t fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* b, int32_t q_heads) {
+size_t fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* b, int32_t q_heads, int32_t weights) {
     if (!kv || !b || q_heads < 1 || q_heads % kv->d.heads || q_heads / kv->d.heads > 128 || b->batch < 1 || b->total_q < 1) return 0;
-    int splits, tiles;
-    attend_splits(b->batch, b->total_q, b->max_len, kv->d.heads, 128 / (q_heads / kv->d.heads), kv->sm_count, &splits, &tiles);
-    return splits > 1 ? (size_t)splits * b->total_q * q_heads * (kv->d.head_dim + 1) * sizeof(float) : 0;
+    const Plan p = plan_attend(kv, b, q_heads, weights != 0);
+    return (p.part_o + p.part_lse + p.scores) * sizeof(float);
 }
 
 fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend_args* x, void* workspace_dev, size_t workspace_bytes, void* cuda_stream,
@@ -288,26 +315,35 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
     a.v_pool = d.v_dev; a.v_page = d.v_page_stride; a.v_token = d.v_token_stride; a.v_head = d.v_head_stride;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     CUtensorMap mq;
+    bool few = false;
     if (b->total_q > 0) {
-        attend_splits(b->batch, b->total_q, b->max_len, d.heads, a.tile_tokens, kv->sm_count, &a.splits, &a.split_tiles);
-        if (a.splits > 1) {
-            const size_t need = (size_t)a.splits * b->total_q * a.q_heads * (d.head_dim + 1) * sizeof(float);
-            if (!workspace_dev || workspace_bytes < need) return err(FD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
-            if (reinterpret_cast<uintptr_t>(workspace_dev) & 15) return err(FD_ERR_INVALID, "workspace must be 16-byte aligned");
-            a.part_o = static_cast<float*>(workspace_dev);
-            a.part_lse = a.part_o + (size_t)a.splits * b->total_q * a.q_heads * d.head_dim;
+        const Plan p = plan_attend(kv, b, a.q_heads, a.w_out != nullptr);
+        const size_t need = (p.part_o + p.part_lse + p.scores) * sizeof(float);
+        if (need && (!workspace_dev || workspace_bytes < need)) return err(FD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+        if (need && (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return err(FD_ERR_INVALID, "workspace must be 16-byte aligned");
+        few = p.few;
+        a.splits = p.splits; a.split_tiles = p.split_tiles;
+        a.part_o = static_cast<float*>(workspace_dev);
+        a.scores = a.part_o + p.part_o; a.score_stride = p.score_stride;
+        a.part_lse = a.scores + p.scores;
+        a.q = heads_of(x->q);
+        cudaError_t e;
+        if (few) {
+            a.box_rows = kv->few_rows;
+            e = launch_few(a, kv->few_k, kv->few_v, stream);
+        } else {
+            const uint64_t dims[3] = {(uint64_t)d.head_dim, (uint64_t)a.q_heads, (uint64_t)b->total_q};
+            const uint32_t box[3] = {64, (uint32_t)a.group, (uint32_t)a.tile_tokens};
+            // (a stride that no step uses may be anything the map accepts)
+            const int64_t strides[2] = {a.q_heads > 1 ? x->q.head_stride : d.head_dim, b->total_q > 1 ? x->q.token_stride : d.head_dim};
+            if (!make_map(&mq, x->q.p_dev, d.dtype, 3, dims, strides, box)) return err(FD_ERR_CUDA, "cuTensorMapEncodeTiled refused q");
+            e = launch_attend(a, mq, kv->map_k, kv->map_v, stream);
         }
-        const uint64_t dims[3] = {(uint64_t)d.head_dim, (uint64_t)a.q_heads, (uint64_t)b->total_q};
-        const uint32_t box[3] = {64, (uint32_t)a.group, (uint32_t)a.tile_tokens};
-        // (a stride that no step uses may be anything the map accepts)
-        const int64_t strides[2] = {a.q_heads > 1 ? x->q.head_stride : d.head_dim, b->total_q > 1 ? x->q.token_stride : d.head_dim};
-        if (!make_map(&mq, x->q.p_dev, d.dtype, 3, dims, strides, box)) return err(FD_ERR_CUDA, "cuTensorMapEncodeTiled refused q");
-        const cudaError_t e = launch_attend(a, mq, kv->map_k, kv->map_v, kv->sm_count, stream);
-        if (e != cudaSuccess) return err.cuda(e, "k_attend");
+        if (e != cudaSuccess) return err.cuda(e, "attention");
     } else {
         mq = kv->map_k;                            // no rows: the weights are copied, nothing is loaded through it
     }
-    if (a.w_out && b->max_len > 0) {
+    if (a.w_out && b->max_len > 0 && !few) {
         const cudaError_t e = launch_weigh(a, mq, kv->map_k, stream);
         if (e != cudaSuccess) return err.cuda(e, "k_weigh");
     }

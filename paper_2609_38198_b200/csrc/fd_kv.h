@@ -10,9 +10,10 @@
 
 struct fd_kv {
     fd_kv_desc d{};
-    int box_rows = 0;                // rows of a page that one TMA box takes: gcd(page_size, 128)
+    int box_rows = 0, few_rows = 0;  // rows of a page that one TMA box takes: gcd(page_size, 128); with few rows gcd(page_size, 16)
     int device = 0, sm_count = 148;
     CUtensorMap map_k, map_v;        // (coordinate, row of the page, head, page)
+    CUtensorMap few_k, few_v;
 };
 
 namespace fd {
@@ -71,22 +72,34 @@ cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream);
 
 struct AttendArgs {
     Batch batch;
-    Heads out;
+    Heads q, out;
     int q_heads, heads, group, head_dim, dtype;
     int tile_tokens;                 // tokens of a 128-row tile: 128 / group; its rows are (token, query head of the group)
     int causal, window;              // window 0: none
     float scale_log2;                // scale * log2(e)
     float* lse;
     const float* w_in; float* w_out; int64_t w_stride;
-    int splits, split_tiles;         // the cache in `splits` parts of split_tiles tiles of 128 tokens
+    int splits, split_tiles;         // the cache in `splits` parts of split_tiles tiles (of 128 tokens; of 64 with few rows)
     float* part_o; float* part_lse;  // [split][token][query head]([head_dim])
+    float* scores; int64_t score_stride;     // few rows and weights: scale_log2 q.k of every row and slot, [sequence][head][kFewRows][score_stride]
     int box_rows;
     const void* v_pool; int64_t v_page, v_token, v_head;
 };
-// How many parts the cache is cut into, and the tiles of each.
-void attend_splits(int batch, int total_q, int max_len, int heads, int tile_tokens, int sm_count, int* splits, int* split_tiles);
-cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int sm_count, cudaStream_t stream);
+// At most this many rows (new tokens x query heads of a group) of a sequence go through the kernel for few rows.
+constexpr int kFewRows = 16;
+
+// How the work of a call is cut, and what its workspace holds.
+struct Plan {
+    bool few;
+    int splits, split_tiles;
+    int64_t score_stride;
+    size_t part_o, part_lse, scores;         // floats
+};
+Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weights);
+cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream);
 cudaError_t launch_weigh(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream);
+cudaError_t launch_few(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream);
+cudaError_t launch_join(const AttendArgs& a, cudaStream_t stream);
 
 }  // namespace kv
 }  // namespace fd

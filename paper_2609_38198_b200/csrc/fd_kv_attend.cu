@@ -16,8 +16,7 @@
 // Every wait is bounded; on expiry the CTA raises a status word, lets its copies land, frees TMEM and exits.
 #include <algorithm>
 
-#include "fd_kv.h"
-#include "fd_tc_common.h"
+#include "fd_kv_dev.h"
 
 namespace fd {
 namespace kv {
@@ -28,17 +27,11 @@ using namespace tc;
 constexpr int kThreadsAt = 384;
 constexpr int kRegsLaunch = 168, kRegsSoft = 216, kRegsUtil = 72;
 static_assert(256 * kRegsSoft + 128 * kRegsUtil <= kThreadsAt * kRegsLaunch, "setmaxnreg must not ask for more than the launch has");
-constexpr float kLazy = 8.0f;            // the running maximum is raised when a score exceeds it by this many powers of two
 
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(smem_u32(smem_dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
-}
-__device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-        ::"r"(smem_u32(smem_dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&v)[32]) {
     asm volatile(
@@ -51,27 +44,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&v)[32]
           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ float max_nan(float a, float b) {       // a NaN is passed on
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-
-template <class T> struct Elem;
-template <> struct Elem<__nv_bfloat16> {
-    static constexpr uint32_t kFormat = 1, kExponent = 0x7f80u;
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        uint32_t r;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-        return r;
-    }
-    static __device__ __forceinline__ float at(const void* p, int64_t i) { return __bfloat162float(((const __nv_bfloat16*)p)[i]); }
-};
-template <> struct Elem<__half> {
-    static constexpr uint32_t kFormat = 0, kExponent = 0x7c00u;
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_f16x2(lo, hi); }
-    static __device__ __forceinline__ float at(const void* p, int64_t i) { return __half2float(((const __half*)p)[i]); }
-};
 // Instruction descriptor, fp32 accumulation, M = 128; `mn`: the B operand is MN-major.
 template <class T> constexpr uint32_t idesc_kv(int n, bool mn) {
     return (1u << 4) | (Elem<T>::kFormat << 7) | (Elem<T>::kFormat << 10) | ((mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
@@ -96,11 +68,6 @@ struct Bars {
     int abort_flag, odd;                                        // odd: elements that are not finite were taken out of a tile
 };
 
-// Which rows a CTA works on: sequence, its first token, what it may see.
-struct Work {
-    int b, begin, count, n;           // sequence, its first row in q, its new tokens, its tokens in the cache
-    int t0;                           // first token of the first tile
-};
 // The slot-th group of `per` tokens of the batch, or b = -1.
 __device__ __forceinline__ Work find_work(const Batch& B, int slot, int per) {
     const int lane = threadIdx.x & 31;
@@ -127,10 +94,6 @@ __device__ __forceinline__ Work find_work(const Batch& B, int slot, int per) {
     }
     return Work{-1, 0, 0, 0, 0};
 }
-// Slots that token t of a sequence sees: [lo, hi).
-__device__ __forceinline__ int see_hi(const AttendArgs& a, const Work& w, int t) { return a.causal ? min(w.n, max(0, w.n - w.count + t + 1)) : w.n; }
-__device__ __forceinline__ int see_lo(const AttendArgs& a, const Work& w, int t) { return a.window ? max(0, w.n - w.count + t + 1 - a.window) : 0; }
-
 // Bits [lo, hi) of a 32-column group that begins at column c.
 __device__ __forceinline__ uint32_t col_mask(int lo, int hi, int c) {
     const int l = min(max(lo - c, 0), 32), h = min(max(hi - c, 0), 32);
@@ -694,11 +657,12 @@ cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorM
     k_attend<T, D><<<(unsigned)(groups * a.heads * a.splits), kThreadsAt, Geo<D>::kSmem, stream>>>(mq, mk, mv, a);
     ++g_launches;
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    if (a.splits > 1) {
-        ++g_launches;
-        e = launch_behind(stream, dim3((unsigned)ceil_div((int64_t)a.batch.total_q * a.q_heads, 8)), dim3(256), 0, k_join<T, D>, a);
-    }
-    return e;
+    return a.splits > 1 ? launch_join(a, stream) : cudaSuccess;
+}
+template <class T, int D>
+cudaError_t join_t(const AttendArgs& a, cudaStream_t stream) {
+    ++g_launches;
+    return launch_behind(stream, dim3((unsigned)ceil_div((int64_t)a.batch.total_q * a.q_heads, 8)), dim3(256), 0, k_join<T, D>, a);
 }
 template <class T, int D>
 cudaError_t weigh_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
@@ -711,23 +675,10 @@ cudaError_t weigh_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMa
 
 }  // namespace
 
-void attend_splits(int batch, int total_q, int max_len, int heads, int tile_tokens, int sm_count, int* splits, int* split_tiles) {
-    // parts of at least two tiles, as many as fill the GPU once if every sequence were as long as the longest
-    const int64_t ctas = ((int64_t)total_q / (2 * tile_tokens) + std::min(batch, total_q)) * heads, tiles = ceil_div(max_len, 128);
-    int64_t s = ctas >= sm_count ? 1 : sm_count / std::max<int64_t>(ctas, 1);
-    s = std::max<int64_t>(1, std::min<int64_t>(s, tiles / 2));
-    const int64_t per = std::max<int64_t>(1, ceil_div(tiles, s));
-    *split_tiles = (int)per;
-    *splits = (int)std::max<int64_t>(1, ceil_div(tiles, per));
-}
-
-#define FD_KV_PICK(fn, ...)                                                                                     \
-    (a.dtype == FD_BF16 ? (a.head_dim == 128 ? fn<__nv_bfloat16, 128>(__VA_ARGS__) : fn<__nv_bfloat16, 64>(__VA_ARGS__)) \
-                        : (a.head_dim == 128 ? fn<__half, 128>(__VA_ARGS__) : fn<__half, 64>(__VA_ARGS__)))
-
-cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int, cudaStream_t stream) {
+cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
     return FD_KV_PICK(attend_t, a, mq, mk, mv, stream);
 }
+cudaError_t launch_join(const AttendArgs& a, cudaStream_t stream) { return FD_KV_PICK(join_t, a, stream); }
 cudaError_t launch_weigh(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
     return FD_KV_PICK(weigh_t, a, mq, mk, stream);
 }

@@ -1,0 +1,56 @@
+// Device code that the attention kernels over paged keys and values share.
+#pragma once
+
+#include "fd_kv.h"
+#include "fd_tc_common.h"
+
+namespace fd {
+namespace kv {
+
+using namespace tc;
+
+constexpr float kLazy = 8.0f;            // the running maximum is raised when a score exceeds it by this many powers of two
+
+__device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ float max_nan(float a, float b) {       // a NaN is passed on
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+template <class T> struct Elem;
+template <> struct Elem<__nv_bfloat16> {
+    static constexpr uint32_t kFormat = 1, kExponent = 0x7f80u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ float at(const void* p, int64_t i) { return __bfloat162float(((const __nv_bfloat16*)p)[i]); }
+};
+template <> struct Elem<__half> {
+    static constexpr uint32_t kFormat = 0, kExponent = 0x7c00u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_f16x2(lo, hi); }
+    static __device__ __forceinline__ float at(const void* p, int64_t i) { return __half2float(((const __half*)p)[i]); }
+};
+
+// Which rows a CTA works on: sequence, its first token, what it may see.
+struct Work {
+    int b, begin, count, n;           // sequence, its first row in q, its new tokens, its tokens in the cache
+    int t0;                           // first token of the first tile
+};
+// Slots that token t of a sequence sees: [lo, hi).
+__device__ __forceinline__ int see_hi(const AttendArgs& a, const Work& w, int t) { return a.causal ? min(w.n, max(0, w.n - w.count + t + 1)) : w.n; }
+__device__ __forceinline__ int see_lo(const AttendArgs& a, const Work& w, int t) { return a.window ? max(0, w.n - w.count + t + 1 - a.window) : 0; }
+
+// Calls fn<element type, head_dim> for the arguments `a`.
+#define FD_KV_PICK(fn, ...)                                                                                     \
+    (a.dtype == FD_BF16 ? (a.head_dim == 128 ? fn<__nv_bfloat16, 128>(__VA_ARGS__) : fn<__nv_bfloat16, 64>(__VA_ARGS__)) \
+                        : (a.head_dim == 128 ? fn<__half, 128>(__VA_ARGS__) : fn<__half, 64>(__VA_ARGS__)))
+
+}  // namespace kv
+}  // namespace fd

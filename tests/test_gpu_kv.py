@@ -410,7 +410,7 @@ def test_attend_refusals(fd):
     from paper_2609_38198_b200 import binding
     qq, oo = randn(1, 1, 4, 64, dtype=BF16), torch.zeros(1, 4, 64, dtype=BF16, device=DEV)
     a = binding.fd_kv_attend_args(binding.fd_heads(qq.data_ptr(), 256, 64, 4), binding.fd_heads(oo.data_ptr(), 256, 64, 4), 0.125, 1, 0)
-    assert fd.lib.fd_kv_attend_bytes(long.cache._h, ctypes.byref(long.batch.struct), 4) > 0
+    assert fd.lib.fd_kv_attend_bytes(long.cache._h, ctypes.byref(long.batch.struct), 4, 0) > 0
     assert short(long.cache._h, ctypes.byref(long.batch.struct), ctypes.byref(a), None, 0, None, None, 0) == fd.FD_ERR_WORKSPACE
 
 

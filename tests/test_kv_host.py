@@ -71,7 +71,7 @@ def test_null_handles(fd):
     assert fd.lib.fd_kv_append(None, ctypes.byref(b), None, None, None, 0) == fd.FD_ERR_INVALID
     assert fd.lib.fd_kv_attend(None, ctypes.byref(b), None, None, 0, None, None, 0) == fd.FD_ERR_INVALID
     assert fd.lib.fd_kv_evict(None, ctypes.byref(b), None, None, None, 0) == fd.FD_ERR_INVALID
-    assert fd.lib.fd_kv_attend_bytes(None, ctypes.byref(b), 8) == 0
+    assert fd.lib.fd_kv_attend_bytes(None, ctypes.byref(b), 8, 0) == 0
     assert fd.lib.fd_kv_synchronize(None, None) == fd.FD_ERR_INVALID
     fd.lib.fd_kv_destroy(None)
 
