@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
@@ -451,17 +452,24 @@ def _heads(t: torch.Tensor, dtype, device, head_dim: int, tokens: int, what: str
     return fd_heads(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d, h)
 
 
+class _Messages(threading.local):
+    def __init__(self):
+        self.buf = ctypes.create_string_buffer(256)
+
+
+_messages = _Messages()
+
+
 def _call(device, fn, *args):
-    """fn(*args, current stream, errbuf, its length) on `device`.  An argument error leaves no launch behind, so the call is made without a buffer for
-    the message and repeated with one when it was refused."""
-    with _on(device):
-        stream = torch._C._cuda_getCurrentRawStream(device.index)
-        st = fn(*args, stream, None, 0)
-        if st != FD_OK:
-            err = ctypes.create_string_buffer(256)
-            if st in (FD_ERR_INVALID, FD_ERR_WORKSPACE, FD_ERR_UNSUPPORTED):
-                fn(*args, stream, err, 256)
-            raise FdError(st, err.value.decode())
+    """fn(*args, current stream, errbuf, its length) on `device`."""
+    err = _messages.buf
+    if torch._C._cuda_getDevice() == device.index:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(device.index), err, 256)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(device.index), err, 256)
+    if st != FD_OK:
+        raise FdError(st, err.value.decode())
 
 
 def fd_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,

@@ -122,6 +122,7 @@ Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weight
         const int64_t ctas = (b->total_q / (2 * (128 / group)) + live) * heads;
         s = std::max<int64_t>(1, std::min(sms / ctas, tiles / 2));
     }
+    s = std::min<int64_t>(s, kMaxSplits);
     p.split_tiles = (int)ceil_div(tiles, s);
     p.splits = (int)ceil_div(tiles, p.split_tiles);
     const size_t rows = (size_t)b->total_q * q_heads;
@@ -213,7 +214,8 @@ fd_status fd_kv_create(fd_kv** out, const fd_kv_desc* d, char* errbuf, size_t er
     if (e != cudaSuccess) { delete kv; return err.cuda(e, "device"); }
     const uint64_t dims[4] = {(uint64_t)d->head_dim, (uint64_t)d->page_size, (uint64_t)d->heads, (uint64_t)d->num_pages};
     const uint32_t box[4] = {64, (uint32_t)kv->box_rows, 1, 1};
-    const uint32_t few[4] = {64, (uint32_t)(kv->few_rows = g < 16 ? g : 16), 1, 1};
+    const int chunk = d->head_dim == 128 ? 16 : 32;
+    const uint32_t few[4] = {64, (uint32_t)(kv->few_rows = g < chunk ? g : chunk), 1, 1};
     const int64_t ks[3] = {d->k_token_stride, d->k_head_stride, d->k_page_stride}, vs[3] = {d->v_token_stride, d->v_head_stride, d->v_page_stride};
     if (!make_map(&kv->map_k, d->k_dev, d->dtype, 4, dims, ks, box) || !make_map(&kv->map_v, d->v_dev, d->dtype, 4, dims, vs, box) ||
         !make_map(&kv->few_k, d->k_dev, d->dtype, 4, dims, ks, few) || !make_map(&kv->few_v, d->v_dev, d->dtype, 4, dims, vs, few)) {
@@ -324,8 +326,8 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
         few = p.few;
         a.splits = p.splits; a.split_tiles = p.split_tiles;
         a.part_o = static_cast<float*>(workspace_dev);
-        a.scores = a.part_o + p.part_o; a.score_stride = p.score_stride;
-        a.part_lse = a.scores + p.scores;
+        a.scores = p.scores ? a.part_o + p.part_o : nullptr; a.score_stride = p.score_stride;
+        a.part_lse = a.part_o + p.part_o + p.scores;
         a.q = heads_of(x->q);
         cudaError_t e;
         if (few) {

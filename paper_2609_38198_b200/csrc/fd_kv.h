@@ -1,5 +1,5 @@
 // Internal declarations of the paged cache's operators (fd_kv.cu: entry points; fd_kv_rows.cu: rotary positions, append, eviction;
-// fd_kv_attend.cu: attention and its column sums).
+// fd_kv_attend.cu: attention and its column sums; fd_kv_decode.cu: attention of few rows; fd_kv_join.cu: what follows both).
 #pragma once
 
 #include <cuda.h>
@@ -10,7 +10,7 @@
 
 struct fd_kv {
     fd_kv_desc d{};
-    int box_rows = 0, few_rows = 0;  // rows of a page that one TMA box takes: gcd(page_size, 128); with few rows gcd(page_size, 16)
+    int box_rows = 0, few_rows = 0;  // rows of a page that one TMA box takes: gcd(page_size, 128); with few rows gcd(page_size, 16 or 32)
     int device = 0, sm_count = 148;
     CUtensorMap map_k, map_v;        // (coordinate, row of the page, head, page)
     CUtensorMap few_k, few_v;
@@ -87,6 +87,7 @@ struct AttendArgs {
 };
 // At most this many rows (new tokens x query heads of a group) of a sequence go through the kernel for few rows.
 constexpr int kFewRows = 16;
+constexpr int kMaxSplits = 1024;         // parts of a cache
 
 // How the work of a call is cut, and what its workspace holds.
 struct Plan {

@@ -24,24 +24,36 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreadsAt = 384;
-constexpr int kRegsLaunch = 168, kRegsSoft = 216, kRegsUtil = 72;
-static_assert(256 * kRegsSoft + 128 * kRegsUtil <= kThreadsAt * kRegsLaunch, "setmaxnreg must not ask for more than the launch has");
+constexpr int kSoftWarps = 8, kThreadsAt = 32 * (kSoftWarps + 4);
+constexpr int kWeighWarps = 16, kThreadsWe = 32 * (kWeighWarps + 3);
+constexpr int kPolyEvery = 0;            // every so many pairs of exponentials are taken on the FMA pipe; 0: none
 
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(smem_u32(smem_dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&v)[32]) {
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
         ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
-          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+// As mbar_wait, for hand-offs inside a tile: polls without backing off.
+__device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned int* status, int code) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    int spins = 0;
+    while (!mbar_try_wait(bar, parity))
+        if ((++spins & 255) == 0) {
+            if (*abort_flag) return false;
+            if (clock64() - t0 > kWaitCycles) {
+                *abort_flag = 1;
+                atomicCAS(status, 0u, (unsigned)(0x100 | code));
+                return false;
+            }
+        }
+    return true;
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // Instruction descriptor, fp32 accumulation, M = 128; `mn`: the B operand is MN-major.
@@ -63,7 +75,7 @@ struct Geo {
 template <int D>
 struct Bars {
     uint64_t q_full, full[Geo<D>::kSlots], empty[Geo<D>::kSlots], clean[Geo<D>::kSlots];
-    uint64_t s_full[2], p_full[2], pv_done[2];
+    uint64_t s_full[2], p_full[2][4], pv_done[2];
     uint32_t tmem_base;
     int abort_flag, odd;                                        // odd: elements that are not finite were taken out of a tile
 };
@@ -139,7 +151,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     const int split = blockIdx.x % a.splits, h = (blockIdx.x / a.splits) % a.heads;
     const int groups = gridDim.x / (a.splits * a.heads), slot = groups - 1 - blockIdx.x / (a.splits * a.heads);
     const int per = 2 * a.tile_tokens;
-    const Work w = find_work(a.batch, slot, per);
+    const Work w = uniform(find_work(a.batch, slot, per));
     if (w.b < 0) return;
     const int t_last = min(w.count, w.t0 + per) - 1;
     const int tiles = (t_last - w.t0) / a.tile_tokens + 1;               // row tiles with work: 1 or 2
@@ -153,11 +165,14 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     if (threadIdx.x == 0) {
         mbar_init(&bars->q_full, 1);
         for (int s = 0; s < G::kSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); mbar_init(&bars->clean[s], 2); }
-        for (int t = 0; t < 2; ++t) { mbar_init(&bars->s_full[t], 1); mbar_init(&bars->p_full[t], 4); mbar_init(&bars->pv_done[t], 1); }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&bars->s_full[t], 1); mbar_init(&bars->pv_done[t], 1);
+            for (int k = 0; k < 4; ++k) mbar_init(&bars->p_full[t][k], 4);
+        }
         bars->abort_flag = 0; bars->odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) {
+    if (warp == kSoftWarps) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -166,9 +181,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
 
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUtil));
-        if (warp == 8 && num > 0) {
+    if (warp >= kSoftWarps) {
+        if (warp == kSoftWarps && num > 0) {
             // ---------------------------------------------------------------- TMA
             const int rows = a.tile_tokens * a.group;
             if (lane == 0) {
@@ -195,7 +209,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 const long long c0 = clock64();
                 while (!mbar_try_wait(&bars->q_full, 0) && clock64() - c0 < 20000000ll) {}
             }
-        } else if (warp == 9 && num > 0) {
+        } else if (warp == kSoftWarps + 1 && num > 0) {
             // ---------------------------------------------------------------- MMA (one thread)
             if (elect_one()) {
                 constexpr uint32_t id_s = idesc_kv<T>(128, false), id_o = idesc_kv<T>(D, true);
@@ -225,15 +239,19 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     ok = mbar_wait(&bars->full[sv], (iv / G::kSlots) & 1, abort_flag, status, 4) &&
                          mbar_wait(&bars->clean[sv], G::value_use(j) & 1, abort_flag, status, 5);
                     for (int t = 0; t < tiles && ok; ++t) {
-                        ok = mbar_wait(&bars->p_full[t], j & 1, abort_flag, status, 6);
-                        if (!ok) break;
-                        tc_fence_after();
                         const uint32_t o_addr = tmem + 256u + (uint32_t)D * t, p_addr = tmem + 128u * t, vt = v_lo + (uint32_t)(sv * G::kTile >> 4);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            if (k == 0 && j == 0) mma_ts2<0>(o_addr, p_addr, vt, hi, id_o);
-                            else mma_ts2<1>(o_addr, p_addr + 8 * k, vt + (uint32_t)(k * 2048 >> 4), hi, id_o);
+                        for (int part = 0; part < 4; ++part) {                  // 32 tokens each
+                            ok = mbar_wait_near(&bars->p_full[t][part], j & 1, abort_flag, status, 6);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int k = 2 * part; k < 2 * part + 2; ++k) {
+                                if (k == 0 && j == 0) mma_ts2<0>(o_addr, p_addr, vt, hi, id_o);
+                                else mma_ts2<1>(o_addr, p_addr + 32 * part + 8 * (k & 1), vt + (uint32_t)(k * 2048 >> 4), hi, id_o);
+                            }
                         }
+                        if (!ok) break;
                         tc_commit(&bars->pv_done[t]);
                         if (j + 1 < num) {
                             if (t == 0) {
@@ -249,7 +267,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     if (j + 1 < num) tc_commit(&bars->empty[sk]);
                 }
             }
-        } else if (warp >= 10 && num > 0) {
+        } else if (num > 0) {
             // ---------------------------------------------------------------- values that some row does not see
             bool ok = true;
             for (int j = 0; j < num; ++j) {
@@ -259,7 +277,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 if (tile < full0 || tile >= full1) {
                     uint8_t* v = ring + sv * G::kTile;
                     bool odd = false;
-                    for (int i = threadIdx.x - 320; i < G::kTile / 16; i += 64) {       // 16 bytes of row (i / 8) % 128; the swizzle stays within the row
+                    for (int i = threadIdx.x - 32 * (kSoftWarps + 2); i < G::kTile / 16; i += 64) {       // 16 bytes of row (i / 8) % 128; the swizzle stays within the row
                         uint4* p = (uint4*)(v + 16 * i);
                         if (tile * 128 + (i / 8) % 128 >= w.n) { *p = make_uint4(0, 0, 0, 0); continue; }
                         uint4 x = *p;
@@ -282,9 +300,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         }
     } else {
         // -------------------------------------------------------------------- softmax (thread = row)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
-        const int t = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const int t = warp >> 2, q = warp & 3, r = q * 32 + lane;
+        const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
         const uint32_t s_addr = tmem + lane_addr + 128u * t, o_addr = tmem + lane_addr + 256u + (uint32_t)D * t;
         const int token = w.t0 + t * a.tile_tokens + r / a.group, head = h * a.group + r % a.group;
         const bool valid = r < a.tile_tokens * a.group && token < w.count;
@@ -296,70 +313,89 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         if (t < tiles) {
             for (int j = 0; j < num; ++j) {
                 const int tile = j0 + j;
-                ok = __all_sync(~0u, mbar_wait(&bars->s_full[t], j & 1, abort_flag, status, 9));
+                ok = __all_sync(~0u, mbar_wait_near(&bars->s_full[t], j & 1, abort_flag, status, 9));
                 if (!ok) break;
-                if (warp_on) {
-                    tc_fence_after();
-                    uint32_t s[4][32];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) tmem_ld32(s_addr + 32 * k, s[k]);
-                    tmem_wait_ld();
-                    if (tile < full0 || tile >= full1) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t see = col_mask(lo, hi, tile * 128 + 32 * k);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (!((see >> i) & 1)) s[k][i] = 0xff800000u;
-                        }
-                    }
-                    float mx[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        mx[k] = __uint_as_float(s[k][0]);
-#pragma unroll
-                        for (int i = 1; i < 32; ++i) mx[k] = max_nan(mx[k], __uint_as_float(s[k][i]));
-                    }
-                    const float top = max_nan(max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3])), m);
-                    const bool raise = !((top - m) * c <= kLazy) && top != m;        // (first tile: from -inf; a NaN goes through)
-                    if (__any_sync(~0u, raise)) {
-                        const float alpha = raise ? ex2f((m - top) * c) : 1.0f;
-                        if (raise) m = top;
-                        l *= alpha;
-                        if (j > 0) {
-                            if (!__all_sync(~0u, mbar_wait(&bars->pv_done[t], (j - 1) & 1, abort_flag, status, 10))) { ok = false; break; }
-                            tc_fence_after();
-#pragma unroll
-                            for (int k = 0; k < D / 32; ++k) {
-                                uint32_t o[32];
-                                tmem_ld32(o_addr + 32 * k, o);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tmem_st32(o_addr + 32 * k, o);
-                            }
-                        }
-                    }
-                    const float mc = m == -INFINITY ? 0.f : m * c;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        uint32_t p[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float x0 = ex2f(fmaf(__uint_as_float(s[2 * k + i / 16][2 * (i % 16)]), c, -mc));
-                            const float x1 = ex2f(fmaf(__uint_as_float(s[2 * k + i / 16][2 * (i % 16) + 1]), c, -mc));
-                            sum[i & 1] += x0; sum[2 + (i & 1)] += x1;
-                            p[i] = Elem<T>::pack(x0, x1);
-                        }
-                        tmem_st32(s_addr + 32 * k, p);
-                    }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tmem_wait_st();
-                    tc_fence_before();
+                if (!warp_on) {
+                    if (lane < 4) mbar_arrive(&bars->p_full[t][lane]);
+                    continue;
                 }
+                tc_fence_after();
+                uint32_t s[4][32];
+                float mx[4];
+                tmem_ld32(s_addr, s[0]);
+                tmem_ld32(s_addr + 32, s[1]);
+                tmem_wait_ld();
+                tmem_ld32(s_addr + 64, s[2]);
+                tmem_ld32(s_addr + 96, s[3]);
+                const bool whole = tile >= full0 && tile < full1;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k == 2) tmem_wait_ld();
+                    if (!whole) {
+                        const uint32_t see = col_mask(lo, hi, tile * 128 + 32 * k);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!((see >> i) & 1)) s[k][i] = 0xff800000u;
+                    }
+                    float y[2];
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        y[z] = max_nan(__uint_as_float(s[k][16 * z]), __uint_as_float(s[k][16 * z + 1]));
+#pragma unroll
+                        for (int i = 2; i < 16; i += 2) y[z] = max_nan(y[z], __uint_as_float(s[k][16 * z + i]), __uint_as_float(s[k][16 * z + i + 1]));
+                    }
+                    mx[k] = max_nan(y[0], y[1]);
+                }
+                const float top = max_nan(max_nan(mx[0], mx[1], mx[2]), mx[3], m);
+                const bool raise = !((top - m) * c <= kLazy) && top != m;        // (first tile: from -inf; a NaN goes through)
+                if (__any_sync(~0u, raise)) {
+                    const float alpha = raise ? ex2f((m - top) * c) : 1.0f;
+                    if (raise) m = top;
+                    l *= alpha;
+                    if (j > 0) {
+                        if (!__all_sync(~0u, mbar_wait_near(&bars->pv_done[t], (j - 1) & 1, abort_flag, status, 10))) { ok = false; break; }
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            uint32_t o[16];
+                            tmem_ld16(o_addr + 16 * k, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st16(o_addr + 16 * k, o);
+                        }
+                        tmem_wait_st();
+                    }
+                }
+                const float mc = m == -INFINITY ? 0.f : m * c;
+                const uint64_t cc = pair2(c, c), mm = pair2(-mc, -mc);
+                uint64_t sum[2] = {0, 0};
+                // 32 tokens at a time: the store of one part completes while the next part's exponentials are taken, then the product may have it
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint64_t x = fma2(pair2(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), cc, mm);
+                        const uint64_t e = kPolyEvery && i % (kPolyEvery ? kPolyEvery : 1) == kPolyEvery - 1 ? ex2_pair(x) : ex2_mufu(x);
+                        sum[i & 1] = add2(sum[i & 1], e);
+                        const float2 v = split2(e);
+                        p[i] = Elem<T>::pack(v.x, v.y);
+                    }
+                    if (k > 0) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bars->p_full[t][k - 1]);
+                    }
+                    tmem_st16(s_addr + 32 * k, p);
+                }
+                const float2 part = split2(add2(sum[0], sum[1]));
+                l += part.x + part.y;
+                tmem_wait_st();
+                tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars->p_full[t]);
+                if (lane == 0) mbar_arrive(&bars->p_full[t][3]);
             }
             if (ok && num > 0) ok = __all_sync(~0u, mbar_wait(&bars->pv_done[t], (num - 1) & 1, abort_flag, status, 11));
         }
@@ -374,21 +410,22 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 else if (a.lse) a.lse[row * a.q_heads + head] = empty ? -INFINITY : (float)((double)(m * c + log2f(l)) * 0.69314718055994530942);
             }
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-                uint32_t u[32];
-                float o[32];
-                if (num > 0) { tmem_ld32(o_addr + 32 * k, u); tmem_wait_ld(); }
+            for (int k = 0; k < D / 16; ++k) {
+                const int d0 = 16 * k;
+                uint32_t u[16];
+                float o[16];
+                if (num > 0) { tmem_ld16(o_addr + d0, u); tmem_wait_ld(); }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = empty ? 0.f : __uint_as_float(u[i]) * inv;
+                for (int i = 0; i < 16; ++i) o[i] = empty ? 0.f : __uint_as_float(u[i]) * inv;
                 if (odd && valid) {
                     // what is not finite in tiles that this CTA's rows see in part, for the rows that see it
                     for (int key = max(lo, j0 * 128); key < min(hi, j1 * 128); ++key) {
                         if (key / 128 >= full0 && key / 128 < full1) { key = full1 * 128 - 1; continue; }
                         const int page = a.batch.table[w.b * a.batch.table_stride + key / a.batch.page_size];
                         if (page < 0 || page >= a.batch.num_pages) continue;
-                        const int64_t at = page * a.v_page + (key % a.batch.page_size) * a.v_token + h * a.v_head + 32 * k;
+                        const int64_t at = page * a.v_page + (key % a.batch.page_size) * a.v_token + h * a.v_head + d0;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
+                        for (int i = 0; i < 16; ++i) {
                             const float v = Elem<T>::at(a.v_pool, at + i);
                             if (!isfinite(v)) o[i] += v;
                         }
@@ -396,13 +433,13 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 }
                 if (valid) {
                     if (a.splits > 1) {
-                        float4* dst = (float4*)(a.part_o + ((split * (int64_t)a.batch.total_q + row) * a.q_heads + head) * D + 32 * k);
+                        float4* dst = (float4*)(a.part_o + ((split * (int64_t)a.batch.total_q + row) * a.q_heads + head) * D + d0);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        for (int i = 0; i < 4; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     } else {
-                        uint4* dst = (uint4*)((T*)a.out.p + row * a.out.token_stride + head * a.out.head_stride + 32 * k);
+                        uint4* dst = (uint4*)((T*)a.out.p + row * a.out.token_stride + head * a.out.head_stride + d0);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 2; ++i)
                             dst[i] = make_uint4(Elem<T>::pack(o[8 * i], o[8 * i + 1]), Elem<T>::pack(o[8 * i + 2], o[8 * i + 3]),
                                                 Elem<T>::pack(o[8 * i + 4], o[8 * i + 5]), Elem<T>::pack(o[8 * i + 6], o[8 * i + 7]));
                     }
@@ -412,49 +449,17 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == kSoftWarps) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
 }
 
-// Joins the parts of the cache: out = sum_s 2^(lse_s - lse) o_s.  One warp a row.
-template <class T, int D>
-__global__ void __launch_bounds__(256) k_join(const AttendArgs a) {
-    grid_wait();
-    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    const int64_t rows = (int64_t)q_begin(a.batch, a.batch.batch) * a.q_heads, all = (int64_t)a.batch.total_q * a.q_heads;
-    if (row >= rows) return;
-    float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = max_nan(top, a.part_lse[s * all + row]);
-    constexpr int E = D / 32;
-    float o[E], sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = 0.f;
-    for (int s = 0; s < a.splits && top != -INFINITY; ++s) {
-        const float part = a.part_lse[s * all + row];
-        if (part == -INFINITY) continue;                       // (its o was not written)
-        const float f = ex2f(part - top);
-        const float* p = a.part_o + (s * all + row) * D + lane * E;
-        sum += f;
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[i] = fmaf(f, p[i], o[i]);
-    }
-    const float inv = top == -INFINITY ? 0.f : 1.0f / sum;
-    const int64_t token = row / a.q_heads;
-    const int head = (int)(row - token * a.q_heads);
-    uint32_t* dst = (uint32_t*)((T*)a.out.p + token * a.out.token_stride + head * a.out.head_stride + lane * E);
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) dst[i] = Elem<T>::pack(o[2 * i] * inv, o[2 * i + 1] * inv);
-    if (a.lse && lane == 0) a.lse[row] = top == -INFINITY ? -INFINITY : (float)((double)(top + log2f(sum)) * 0.69314718055994530942);
-}
-
 // k_weigh: what every cached token received, w_j += sum over rows of 2^(c s - lse).  One CTA takes two tiles of 128 cached tokens as the M side (S^T = K Q^T: a
 // thread owns a token, so the sum over rows is a sum over its columns and needs no exchange) and goes through the rows that see them.
-constexpr int kWeighSlots = 3;
+constexpr int kWeighSlots = 3, kWeighPoly = 0;
 template <int D>
 struct WeighSmem {
-    static constexpr int kBytes = 1024 + (2 + kWeighSlots) * Geo<D>::kTile + 4 * 128 * 4 + 512;
+    static constexpr int kBytes = 1024 + (2 + kWeighSlots) * Geo<D>::kTile + 4 * 128 * 4 + 2 * 128 * 4 + 512;
 };
 struct WeighBars {
     uint64_t k_full, full[kWeighSlots], empty[kWeighSlots], s_full[2][2], s_empty[2][2], l_full[4];
@@ -463,7 +468,7 @@ struct WeighBars {
 };
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreadsAt, 1)
+__global__ void __launch_bounds__(kThreadsWe, 1)
 k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const AttendArgs a) {
     using G = Geo<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -471,13 +476,15 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     uint8_t* k_base = base;
     uint8_t* ring = base + 2 * G::kTile;
     float* l_ring = (float*)(ring + kWeighSlots * G::kTile);                  // [4][128]: -lse of a row tile, -inf for rows that are none
-    WeighBars* bars = (WeighBars*)(l_ring + 4 * 128);
+    float* s_acc = l_ring + 4 * 128;                                          // [tile][token]: sums of the second column halves
+    WeighBars* bars = (WeighBars*)(s_acc + 2 * 128);
     volatile int* abort_flag = &bars->abort_flag;
     unsigned int* status = a.batch.status + 1;
 
     const int h = blockIdx.y, b = blockIdx.z, key0 = blockIdx.x * 256;
     Work w;
     w.b = b; w.begin = q_begin(a.batch, b); w.count = max(0, q_begin(a.batch, b + 1) - w.begin); w.n = kv_length(a.batch, b, false); w.t0 = 0;
+    w = uniform(w);
     if (key0 >= w.n) return;
     const int tiles = w.n - key0 > 128 ? 2 : 1, key_last = min(w.n, key0 + 256) - 1, off = w.n - w.count;
     // tokens that see one of these slots: [ta, tb)
@@ -486,14 +493,16 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     const int rows = a.tile_tokens * a.group;
 
     const int warp = warp_index(), lane = threadIdx.x & 31;
+    const int key = key0 + ((warp >> 2) & 1) * 128 + (warp & 3) * 32 + lane;          // of the first 16 warps
+    float acc = 0.f;
     if (threadIdx.x == 0) {
         mbar_init(&bars->k_full, 1);
         for (int s = 0; s < kWeighSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
-        for (int i = 0; i < 4; ++i) { mbar_init(&bars->s_full[i >> 1][i & 1], 1); mbar_init(&bars->s_empty[i >> 1][i & 1], 4); mbar_init(&bars->l_full[i], 1); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&bars->s_full[i >> 1][i & 1], 1); mbar_init(&bars->s_empty[i >> 1][i & 1], 8); mbar_init(&bars->l_full[i], 1); }
         bars->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) {
+    if (warp == kWeighWarps) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -502,7 +511,7 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
 
-    if (warp == 8 && num > 0) {
+    if (warp == kWeighWarps && num > 0) {
         // -------------------------------------------------------------------- TMA
         bool ok = true;
         {   // both key tiles arrive on one barrier: bytes first, then the copies
@@ -542,7 +551,7 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
                 while (!mbar_try_wait(&bars->k_full, 0) && clock64() - c0 < 20000000ll) {}
             }
         }
-    } else if (warp == 9 && num > 0) {
+    } else if (warp == kWeighWarps + 1 && num > 0) {
         // -------------------------------------------------------------------- MMA (one thread)
         if (elect_one()) {
             constexpr uint32_t id = idesc_kv<T>(128, false);
@@ -568,7 +577,7 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
                 if (ok) tc_commit(&bars->empty[s]);
             }
         }
-    } else if (warp == 10 && num > 0) {
+    } else if (warp == kWeighWarps + 2 && num > 0) {
         // -------------------------------------------------------------------- -lse of each row tile, in powers of two
         bool ok = true;
         for (int i = 0; i < num; ++i) {
@@ -592,56 +601,73 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->l_full[i & 3]);
         }
-    } else if (warp < 8) {
-        const int t = warp >> 2, key = key0 + t * 128 + (warp & 3) * 32 + lane;
+    } else if (warp < kWeighWarps) {
+        // -------------------------------------------------------------------- a thread owns a token and half of the rows
+        const int t = (warp >> 2) & 1, half = warp >> 3;
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-        float acc0 = 0.f, acc1 = 0.f;
         bool ok = true;
         if (t < tiles) {
             for (int i = 0; i < num; ++i) {
                 const int buf = i & 1, tok0 = (q0 + i) * a.tile_tokens;
                 ok = __all_sync(~0u, mbar_wait(&bars->l_full[i & 3], (i >> 2) & 1, abort_flag, status, 26) &&
-                                     mbar_wait(&bars->s_full[t][buf], (i >> 1) & 1, abort_flag, status, 27));
+                                     mbar_wait_near(&bars->s_full[t][buf], (i >> 1) & 1, abort_flag, status, 27));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t addr = tmem + lane_addr + 256u * t + 128u * buf;
-                const float* lr = l_ring + (i & 3) * 128;
+                const uint32_t addr = tmem + lane_addr + 256u * t + 128u * buf + 64u * half;
+                const float* lr = l_ring + (i & 3) * 128 + 64 * half;
                 // columns of rows that see this token: [cl, ch)
                 const int valid = min(rows, (w.count - tok0) * a.group);
                 int cl = 0, ch = valid;
                 if (a.causal) cl = max(0, key - off - tok0) * a.group;
                 if (a.window) ch = (int)min((int64_t)valid, max((int64_t)0, (int64_t)key - off + a.window - tok0) * a.group);
                 const bool whole = __all_sync(~0u, cl == 0 && ch >= 128);
-                for (int k = 0; k < 4 && 32 * k < valid; ++k) {
-                    uint32_t s[32];
-                    tmem_ld32(addr + 32 * k, s);
-                    tmem_wait_ld();
-                    const uint32_t see = whole ? 0xffffffffu : col_mask(cl, ch, 32 * k);
-                    float p[32];
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) p[x] = ex2f(fmaf(__uint_as_float(s[x]), a.scale_log2, lr[32 * k + x]));
-                    if (!whole)
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) if (!((see >> x) & 1)) p[x] = 0.f;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) sum[x & 3] += p[x];
-                    acc0 += sum[0] + sum[1];
-                    acc1 += sum[2] + sum[3];
-                }
+                const uint64_t cc = pair2(a.scale_log2, a.scale_log2);
+                uint32_t s[2][32];
+                tmem_ld32(addr, s[0]);
+                tmem_ld32(addr + 32, s[1]);
+                tmem_wait_ld();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars->s_empty[t][buf]);
+                if (whole) {
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int x = 0; x < 32; x += 4) {
+                            const float4 lv = *(const float4*)(lr + 32 * k + x);
+                            const uint64_t e0 = fma2(pair2(__uint_as_float(s[k][x]), __uint_as_float(s[k][x + 1])), cc, pair2(lv.x, lv.y));
+                            const uint64_t e1 = fma2(pair2(__uint_as_float(s[k][x + 2]), __uint_as_float(s[k][x + 3])), cc, pair2(lv.z, lv.w));
+                            sum[0] = add2(sum[0], ex2_mufu(e0));
+                            sum[1] = add2(sum[1], kWeighPoly && x % (4 * (kWeighPoly ? kWeighPoly : 1)) == 0 ? ex2_pair(e1) : ex2_mufu(e1));
+                        }
+                    const float2 p = split2(add2(sum[0], sum[1]));
+                    acc += p.x + p.y;
+                } else if (64 * half < valid) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t see = col_mask(cl, ch, 64 * half + 32 * k);
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) {
+                            const float p = ex2f(fmaf(__uint_as_float(s[k][x]), a.scale_log2, lr[32 * k + x]));
+                            sum[x & 3] += (see >> x) & 1 ? p : 0.f;
+                        }
+                        acc += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    }
+                }
             }
-            if (ok && key < w.n) {
-                const int64_t at = ((int64_t)b * a.heads + h) * a.w_stride + key;
-                a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + (acc0 + acc1);
-            }
+            if (!ok) acc = 0.f;
         }
+        if (half) s_acc[t * 128 + (warp & 3) * 32 + lane] = acc;
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp < 8 && key < w.n && !*abort_flag) {
+        const int64_t at = ((int64_t)b * a.heads + h) * a.w_stride + key;
+        a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + (acc + s_acc[key - key0]);
+    }
+    if (warp == kWeighWarps) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
 }
@@ -650,9 +676,6 @@ template <class T, int D>
 cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
     cudaError_t e = cudaFuncSetAttribute(k_attend<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<D>::kSmem);
     if (e != cudaSuccess) return e;
-    cudaFuncAttributes fa;
-    if ((e = cudaFuncGetAttributes(&fa, k_attend<T, D>)) != cudaSuccess) return e;
-    if (fa.numRegs != kRegsLaunch) return cudaErrorInvalidKernelImage;             // the split of the registers counts on it
     const int64_t groups = a.batch.total_q / (2 * a.tile_tokens) + std::min(a.batch.batch, a.batch.total_q);
     k_attend<T, D><<<(unsigned)(groups * a.heads * a.splits), kThreadsAt, Geo<D>::kSmem, stream>>>(mq, mk, mv, a);
     ++g_launches;
@@ -660,15 +683,10 @@ cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorM
     return a.splits > 1 ? launch_join(a, stream) : cudaSuccess;
 }
 template <class T, int D>
-cudaError_t join_t(const AttendArgs& a, cudaStream_t stream) {
-    ++g_launches;
-    return launch_behind(stream, dim3((unsigned)ceil_div((int64_t)a.batch.total_q * a.q_heads, 8)), dim3(256), 0, k_join<T, D>, a);
-}
-template <class T, int D>
 cudaError_t weigh_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
     cudaError_t e = cudaFuncSetAttribute(k_weigh<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeighSmem<D>::kBytes);
     if (e != cudaSuccess) return e;
-    k_weigh<T, D><<<dim3((unsigned)ceil_div(a.batch.max_len, 256), a.heads, a.batch.batch), kThreadsAt, WeighSmem<D>::kBytes, stream>>>(mq, mk, a);
+    k_weigh<T, D><<<dim3((unsigned)ceil_div(a.batch.max_len, 256), a.heads, a.batch.batch), kThreadsWe, WeighSmem<D>::kBytes, stream>>>(mq, mk, a);
     ++g_launches;
     return cudaGetLastError();
 }
@@ -678,7 +696,6 @@ cudaError_t weigh_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMa
 cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
     return FD_KV_PICK(attend_t, a, mq, mk, mv, stream);
 }
-cudaError_t launch_join(const AttendArgs& a, cudaStream_t stream) { return FD_KV_PICK(join_t, a, stream); }
 cudaError_t launch_weigh(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
     return FD_KV_PICK(weigh_t, a, mq, mk, stream);
 }

@@ -2,10 +2,10 @@
 //
 // k_few.  A sequence has at most 16 rows (new token, query head of the group) per cached head, so a tile of tcgen05 would be 7/8 padding and, worse, every 128
 // tokens would wait for the chain product -> TMEM -> softmax -> TMEM -> product.  Here each warp goes its own way: it takes every fourth chunk of 16
-// tokens of the CTA's part, keeps several chunks of keys and values in flight by TMA in a ring of its own (no barrier between warps),
+// tokens of the CTA's part (32 where a row has 64 coordinates), keeps several chunks of keys and values in flight by TMA in a ring of its own (no barrier between warps),
 // multiplies with mma.sync m16n8k16 out of ldmatrix fragments and holds scores, weights and the 16 x D result in registers.  Two CTAs of four warps an SM
 // keep 192 KB in flight.  The warps' results are joined in shared memory at the end, the parts of a cache by k_join.
-// With weights wanted, each row's scaled scores go to the workspace (4 bytes a row and token, beside 4 D bytes of keys and values), and k_few_weigh
+// With weights wanted, each row's scaled scores go to the workspace (4 bytes a row and token, beside 4 D bytes of keys and values), and k_join
 // turns them into weights once the norm is known: the keys are not read again.
 #include <algorithm>
 
@@ -19,8 +19,9 @@ constexpr int kWarpsFew = 4;
 
 template <int D>
 struct GeoFew {
-    static constexpr int kStages = D == 128 ? 3 : 6;
-    static constexpr int kHalf = 16 * 128;                       // 16 tokens x 64 coordinates
+    static constexpr int kKeys = D == 128 ? 16 : 32;             // tokens of a chunk: 8 KB of keys and values
+    static constexpr int kStages = 3;
+    static constexpr int kHalf = kKeys * 128;                    // 64 coordinates of a chunk
     static constexpr int kTile = (D / 64) * kHalf;               // keys or values of a chunk
     static constexpr int kSmem = 1024 + kWarpsFew * kStages * 2 * kTile + 256 + kWarpsFew * 16 * 8;
     static_assert(kWarpsFew * 16 * D * 4 <= kWarpsFew * kStages * 2 * kTile, "the warps' results fit in the ring");
@@ -78,10 +79,12 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
         return;
     }
     w.n = kv_length(a.batch, b, threadIdx.x == 0);
+    w = uniform(w);
+    constexpr int KEYS = G::kKeys, NT = KEYS / 8;
     const int rows = w.count * a.group, part = a.split_tiles * 64;
     const int k0 = max(see_lo(a, w, 0), split * part), k1 = a.splits > 1 ? min(see_hi(a, w, w.count - 1), (split + 1) * part) : see_hi(a, w, w.count - 1);
     const int full0 = see_lo(a, w, w.count - 1), full1 = see_hi(a, w, 0);          // every row sees [full0, full1)
-    const int c0 = k0 / 16, chunks = max(0, (k1 + 15) / 16 - c0);
+    const int c0 = k0 / KEYS, chunks = max(0, (k1 + KEYS - 1) / KEYS - c0);
     const int mine = chunks > warp ? (chunks - warp + kWarpsFew - 1) / kWarpsFew : 0;
 
     if (threadIdx.x == 0) {
@@ -93,33 +96,29 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
 
     uint8_t* ring = base + warp * G::kStages * 2 * G::kTile;
     uint64_t* full = bars + warp * G::kStages;
-    int page0 = 0, page1 = 0;                                        // of the chunk 32 (i / 32) + lane: pages of its (one or two) boxes
+    const int boxes = KEYS / a.box_rows;                             // 1, 2 or 4 a chunk
+    int page = 0;                                                    // of box 32 k + lane of this warp's boxes, all chunks in a row
     auto issue = [&](int i) {
-        if ((i & 31) == 0) {
-            const int key = (c0 + warp + kWarpsFew * (i + lane)) * 16;
-            auto page = [&](int k) {
-                if (i + lane >= mine || k >= w.n) return 0;
-                int p = a.batch.table[b * a.batch.table_stride + k / a.batch.page_size];
-                if (p < 0 || p >= a.batch.num_pages) { p = a.batch.num_pages; atomicOr(a.batch.status, kBadPage); }   // (outside: TMA fills with zeros)
-                return p;
-            };
-            page0 = page(key);
-            page1 = a.box_rows == 16 ? 0 : page(key + 8);
+        const int e = i * boxes;
+        if ((e & 31) == 0) {
+            const int ii = (e + lane) / boxes, key = (c0 + warp + kWarpsFew * ii) * KEYS + ((e + lane) % boxes) * a.box_rows;
+            page = 0;
+            if (ii < mine && key < w.n) {
+                page = a.batch.table[b * a.batch.table_stride + key / a.batch.page_size];
+                if (page < 0 || page >= a.batch.num_pages) { page = a.batch.num_pages; atomicOr(a.batch.status, kBadPage); }   // (outside: TMA fills with zeros)
+            }
         }
-        const int p0 = __shfl_sync(~0u, page0, i & 31), p1 = __shfl_sync(~0u, page1, i & 31);
-        if (lane == 0) {
-            const int key = (c0 + warp + kWarpsFew * i) * 16, st = i % G::kStages;
-            uint8_t* k = ring + st * 2 * G::kTile;
-            const int two = a.box_rows == 8 && key + 8 < w.n;
-            mbar_expect_tx(&full[st], (uint32_t)(a.box_rows * (1 + two) * D * 4));
+        const int at = __shfl_sync(~0u, page, (e + lane) & 31), st = i % G::kStages;
+        const int key0 = (c0 + warp + kWarpsFew * i) * KEYS, key = key0 + lane * a.box_rows;
+        const int live = min(boxes, (w.n - key0 + a.box_rows - 1) / a.box_rows);
+        uint8_t* k = ring + st * 2 * G::kTile;
+        if (lane == 0) mbar_expect_tx(&full[st], (uint32_t)(live * a.box_rows * D * 4));
+        __syncwarp();
+        if (lane < live) {
 #pragma unroll
             for (int x = 0; x < D / 64; ++x) {
-                tma_load_4d(k + x * G::kHalf, &map_k, x * 64, key % a.batch.page_size, h, p0, &full[st]);
-                tma_load_4d(k + G::kTile + x * G::kHalf, &map_v, x * 64, key % a.batch.page_size, h, p0, &full[st]);
-                if (two) {
-                    tma_load_4d(k + x * G::kHalf + 1024, &map_k, x * 64, (key + 8) % a.batch.page_size, h, p1, &full[st]);
-                    tma_load_4d(k + G::kTile + x * G::kHalf + 1024, &map_v, x * 64, (key + 8) % a.batch.page_size, h, p1, &full[st]);
-                }
+                tma_load_4d(k + x * G::kHalf + lane * a.box_rows * 128, &map_k, x * 64, key % a.batch.page_size, h, at, &full[st]);
+                tma_load_4d(k + G::kTile + x * G::kHalf + lane * a.box_rows * 128, &map_v, x * 64, key % a.batch.page_size, h, at, &full[st]);
             }
         }
         __syncwarp();
@@ -162,22 +161,28 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
 
     int i = 0;
     for (; i < mine; ++i) {
-        const int st = i % G::kStages, key = (c0 + warp + kWarpsFew * i) * 16;
+        const int st = i % G::kStages, key = (c0 + warp + kWarpsFew * i) * KEYS;
         ok = __all_sync(~0u, mbar_wait(&full[st], (i / G::kStages) & 1, abort_flag, status, 41));
         if (!ok) break;
         const uint32_t ks = smem_u32(ring + st * 2 * G::kTile), vs = ks + G::kTile;
-        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        float s[NT][4];
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            uint32_t f[4];
-            ldmatrix4<false>(f, ks + (k / 4) * G::kHalf + krow + ((uint32_t)(((k % 4) * 2 + (mi & 1)) ^ mr) << 4));
-            mma16816<T>(s[0], qf[k], f[0], f[1]);
-            mma16816<T>(s[1], qf[k], f[2], f[3]);
-        }
-        const bool whole = key >= full0 && key + 16 <= full1;
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int n = 0; n < NT; n += 2) {
+                uint32_t f[4];
+                ldmatrix4<false>(f, ks + (k / 4) * G::kHalf + n * 1024 + krow + ((uint32_t)(((k % 4) * 2 + (mi & 1)) ^ mr) << 4));
+                mma16816<T>(s[n], qf[k], f[0], f[1]);
+                mma16816<T>(s[n + 1], qf[k], f[2], f[3]);
+            }
+        const bool whole = key >= full0 && key + KEYS <= full1;
         if (!whole) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = key + 8 * n + 2 * t + (e & 1);
@@ -187,14 +192,16 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
 #pragma unroll
         for (int r = 0; r < 2; ++r)
             if (score_row[r]) {
-                *(float2*)(score_row[r] + key) = make_float2(s[0][2 * r] * c, s[0][2 * r + 1] * c);
-                *(float2*)(score_row[r] + key + 8) = make_float2(s[1][2 * r] * c, s[1][2 * r + 1] * c);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) *(float2*)(score_row[r] + key + 8 * n) = make_float2(s[n][2 * r] * c, s[n][2 * r + 1] * c);
             }
         float top[2];
         bool raise = false;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            top[r] = max_nan(max_nan(max_nan(s[0][2 * r], s[0][2 * r + 1]), max_nan(s[1][2 * r], s[1][2 * r + 1])), m[r]);
+            top[r] = m[r];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) top[r] = max_nan(top[r], s[n][2 * r], s[n][2 * r + 1]);
             raise |= !((top[r] - m[r]) * c <= kLazy) && top[r] != m[r];
         }
         if (__any_sync(~0u, raise)) {
@@ -209,34 +216,27 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                 for (int n = 0; n < D / 8; ++n) { o[n][2 * r] *= f; o[n][2 * r + 1] *= f; }
             }
         }
-        uint32_t p[4];
+        uint32_t p[NT / 2][4];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const float mc = m[r] == -INFINITY ? 0.f : m[r] * c;
-            float e[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) e[x] = ex2f(fmaf(s[x >> 1][2 * r + (x & 1)], c, -mc));
-            l[r] += (e[0] + e[1]) + (e[2] + e[3]);
-            p[r] = Elem<T>::pack(e[0], e[1]);
-            p[2 + r] = Elem<T>::pack(e[2], e[3]);
-        }
-        if (whole) {
-#pragma unroll
-            for (int n = 0; n < D / 16; ++n) {
-                uint32_t f[4];
-                ldmatrix4<true>(f, vs + (n / 4) * G::kHalf + vrow + ((uint32_t)(((n % 4) * 2 + (mi >> 1)) ^ mr) << 4));
-                mma16816<T>(o[2 * n], p, f[0], f[1]);
-                mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
+            for (int n = 0; n < NT; ++n) {
+                const float e0 = ex2f(fmaf(s[n][2 * r], c, -mc)), e1 = ex2f(fmaf(s[n][2 * r + 1], c, -mc));
+                l[r] += e0 + e1;
+                p[n / 2][2 * (n % 2) + r] = Elem<T>::pack(e0, e1);
             }
-        } else {
-            const int left0 = min(max(w.n - (key + 2 * t), 0), 2), left1 = min(max(w.n - (key + 8 + 2 * t), 0), 2);
+        }
+#pragma unroll
+        for (int x = 0; x < KEYS / 16; ++x) {
+            const int left0 = min(max(w.n - (key + 16 * x + 2 * t), 0), 2), left1 = min(max(w.n - (key + 16 * x + 8 + 2 * t), 0), 2);
 #pragma unroll
             for (int n = 0; n < D / 16; ++n) {
                 uint32_t f[4];
-                ldmatrix4<true>(f, vs + (n / 4) * G::kHalf + vrow + ((uint32_t)(((n % 4) * 2 + (mi >> 1)) ^ mr) << 4));
-                odd |= clean<T>(f[0], left0) | clean<T>(f[1], left1) | clean<T>(f[2], left0) | clean<T>(f[3], left1);
-                mma16816<T>(o[2 * n], p, f[0], f[1]);
-                mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
+                ldmatrix4<true>(f, vs + (n / 4) * G::kHalf + x * 2048 + vrow + ((uint32_t)(((n % 4) * 2 + (mi >> 1)) ^ mr) << 4));
+                if (!whole) odd |= clean<T>(f[0], left0) | clean<T>(f[1], left1) | clean<T>(f[2], left0) | clean<T>(f[3], left1);
+                mma16816<T>(o[2 * n], p[x], f[0], f[1]);
+                mma16816<T>(o[2 * n + 1], p[x], f[2], f[3]);
             }
         }
         __syncwarp();
@@ -292,8 +292,8 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
         if (any_odd) {
             // what is not finite among tokens that some row does not see, for the rows that see it
             for (int key = max(see_lo(a, w, token), k0); key < min(see_hi(a, w, token), k1); ++key) {
-                const int chunk = key & ~15;
-                if (chunk >= full0 && chunk + 16 <= full1) continue;
+                const int chunk = key / KEYS * KEYS;
+                if (chunk >= full0 && chunk + KEYS <= full1) continue;
                 const int page = a.batch.table[b * a.batch.table_stride + key / a.batch.page_size];
                 if (page < 0 || page >= a.batch.num_pages) continue;
                 const int64_t from = page * a.v_page + (key % a.batch.page_size) * a.v_token + h * a.v_head + d;
@@ -316,28 +316,6 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
     }
 }
 
-// w_j += sum over the rows that see token j of 2^(score - lse), from the scores k_few left.  One thread a token.
-__global__ void __launch_bounds__(256) k_few_weigh(const AttendArgs a) {
-    grid_wait();
-    const int h = blockIdx.y, b = blockIdx.z, key = blockIdx.x * 256 + threadIdx.x;
-    Work w;
-    w.b = b; w.begin = q_begin(a.batch, b); w.count = max(0, q_begin(a.batch, b + 1) - w.begin); w.t0 = 0;
-    w.n = kv_length(a.batch, b, false);
-    if (key >= w.n) return;
-    float sum = 0.f;
-    if (w.count <= kFewRows / a.group) {
-        const float* s = a.scores + ((int64_t)b * a.heads + h) * kFewRows * a.score_stride + key;
-        for (int r = 0; r < w.count * a.group; ++r) {
-            const int token = r / a.group;
-            if (key < see_lo(a, w, token) || key >= see_hi(a, w, token)) continue;
-            const float lse = a.lse[(int64_t)(w.begin + token) * a.q_heads + h * a.group + r % a.group];
-            sum += ex2f(s[r * a.score_stride] - (float)((double)lse * 1.44269504088896340736));
-        }
-    }
-    const int64_t at = ((int64_t)b * a.heads + h) * a.w_stride + key;
-    a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
-}
-
 template <class T, int D>
 cudaError_t few_t(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
     cudaError_t e = cudaFuncSetAttribute(k_few<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, GeoFew<D>::kSmem);
@@ -345,12 +323,7 @@ cudaError_t few_t(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap&
     k_few<T, D><<<(unsigned)((int64_t)a.batch.batch * a.heads * a.splits), kWarpsFew * 32, GeoFew<D>::kSmem, stream>>>(mk, mv, a);
     ++g_launches;
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    if (a.splits > 1 && (e = launch_join(a, stream)) != cudaSuccess) return e;
-    if (a.w_out && a.batch.max_len > 0) {
-        ++g_launches;
-        e = launch_behind(stream, dim3((unsigned)ceil_div(a.batch.max_len, 256), a.heads, a.batch.batch), dim3(256), 0, k_few_weigh, a);
-    }
-    return e;
+    return a.splits > 1 || a.w_out ? launch_join(a, stream) : cudaSuccess;
 }
 
 }  // namespace

@@ -22,6 +22,38 @@ __device__ __forceinline__ float max_nan(float a, float b) {       // a NaN is p
     return r;
 }
 
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// 2^x of a pair on the FMA pipe, as tc::ex2_fma2, except that a NaN comes through: the power of two is multiplied in instead of being added to the exponent.
+__device__ __forceinline__ uint64_t ex2_pair(uint64_t x) {
+    constexpr float kRound = 12582912.0f;
+    const float2 c = split2(x);
+    x = pair2(max_nan(c.x, -126.0f), max_nan(c.y, -126.0f));
+    const uint64_t t = add2(x, pair2(kRound, kRound));
+    const uint64_t f = sub2(x, add2(t, pair2(-kRound, -kRound)));
+    uint64_t q = pair2(0.00015353363f, 0.00015353363f);
+    q = fma2(q, f, pair2(0.0013398875f, 0.0013398875f));
+    q = fma2(q, f, pair2(0.009618437f, 0.009618437f));
+    q = fma2(q, f, pair2(0.055503324f, 0.055503324f));
+    q = fma2(q, f, pair2(0.24022648f, 0.24022648f));
+    q = fma2(q, f, pair2(0.6931472f, 0.6931472f));
+    q = fma2(q, f, pair2(1.0f, 1.0f));
+    const float2 ts = split2(t);
+    return mul2(q, pair2(__int_as_float((__float_as_int(ts.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(ts.y) << 23) + 0x3f800000)));
+}
+__device__ __forceinline__ uint64_t ex2_mufu(uint64_t x) {
+    const float2 c = split2(x);
+    return pair2(ex2f(c.x), ex2f(c.y));
+}
+
 template <class T> struct Elem;
 template <> struct Elem<__nv_bfloat16> {
     static constexpr uint32_t kFormat = 1, kExponent = 0x7f80u;
@@ -43,6 +75,10 @@ struct Work {
     int b, begin, count, n;           // sequence, its first row in q, its new tokens, its tokens in the cache
     int t0;                           // first token of the first tile
 };
+// The same value in a register that the compiler knows to be the same for the whole warp: loops and addresses made of it stay in uniform registers, without which
+// every MMA that a thread issues costs about 45 clocks (tc::elect_one).
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ Work uniform(const Work& w) { return Work{uniform(w.b), uniform(w.begin), uniform(w.count), uniform(w.n), uniform(w.t0)}; }
 // Slots that token t of a sequence sees: [lo, hi).
 __device__ __forceinline__ int see_hi(const AttendArgs& a, const Work& w, int t) { return a.causal ? min(w.n, max(0, w.n - w.count + t + 1)) : w.n; }
 __device__ __forceinline__ int see_lo(const AttendArgs& a, const Work& w, int t) { return a.window ? max(0, w.n - w.count + t + 1 - a.window) : 0; }

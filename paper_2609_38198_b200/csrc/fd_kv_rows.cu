@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
             if (q_begin(B, mid) <= t) lo = mid; else hi = mid;
         }
         const int begin = q_begin(B, lo), end = q_begin(B, lo + 1);
-        place[threadIdx.x][0] = -1;
+        place[threadIdx.x][0] = place[threadIdx.x][1] = -1;
         if (t >= begin && t < end) {
             const int n = kv_length(B, lo, true), slot = n - (end - begin) + (t - begin);
             const int page = slot < 0 ? -1 : B.table[lo * B.table_stride + slot / B.page_size];
@@ -62,11 +62,15 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
     __syncthreads();
     const int unit_count = a.head_dim / (2 * VEC), turned = a.rot / (2 * VEC);
     const int heads = a.x.heads + (a.append ? a.k.heads + a.v.heads : 0);
-    const int items = nt * heads * unit_count;
-    for (int i = threadIdx.x + blockIdx.y * kRowThreads; i < items; i += kRowThreads * gridDim.y) {
-        const int hu = i / unit_count, u = i - hu * unit_count;
-        const int t = hu / heads;
-        int h = hu - t * heads;
+    // this thread's units: (token, head, unit) numbers `me`, me + all, ...; they advance without divisions
+    const int all = kRowThreads * gridDim.y, me = threadIdx.x + blockIdx.y * kRowThreads;
+    int u = me % unit_count, h = me / unit_count, t = h / heads;
+    h -= t * heads;
+    const int du = all % unit_count, dh = (all / unit_count) % heads, dt = all / unit_count / heads;
+    for (; t < nt; u += du, h += dh, t += dt) {
+        if (u >= unit_count) { u -= unit_count; ++h; }
+        if (h >= heads) { h -= heads; ++t; }
+        if (t >= nt) break;
         const T* src;
         T* dst;
         bool rot = u < turned;
@@ -74,15 +78,15 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
             src = (const T*)a.x.p + (t0 + t) * a.x.token_stride + h * a.x.head_stride;
             dst = (T*)a.y.p + (t0 + t) * a.y.token_stride + h * a.y.head_stride;
         } else {
-            h -= a.x.heads;
+            int k = h - a.x.heads;
             if (place[t][0] < 0) continue;
-            if (h < a.k.heads) {
-                src = (const T*)a.k.p + (t0 + t) * a.k.token_stride + h * a.k.head_stride;
-                dst = (T*)a.k_pool + place[t][0] + h * a.k_head;
+            if (k < a.k.heads) {
+                src = (const T*)a.k.p + (t0 + t) * a.k.token_stride + k * a.k.head_stride;
+                dst = (T*)a.k_pool + place[t][0] + k * a.k_head;
             } else {
-                h -= a.k.heads;
-                src = (const T*)a.v.p + (t0 + t) * a.v.token_stride + h * a.v.head_stride;
-                dst = (T*)a.v_pool + place[t][1] + h * a.v_head;
+                k -= a.k.heads;
+                src = (const T*)a.v.p + (t0 + t) * a.v.token_stride + k * a.v.head_stride;
+                dst = (T*)a.v_pool + place[t][1] + k * a.v_head;
                 rot = false;
             }
         }
@@ -154,11 +158,12 @@ cudaError_t launch_rows_any(const RowsArgs& a, int sm_count, cudaStream_t stream
 }
 
 // ------------------------------------------------------------------------------------------------ eviction
-// k_select: one block per (sequence, head).  The weights of the middle tokens are mapped to unsigned keys of the same order; four passes of 8
-// bits find the key of rank m from the top, and a last pass in slot order writes down the kept slots (all keys above it, the
-// first of those equal to it).  Slots and weights are read before the positions they move to are written: a kept slot moves down only,
-// never beyond the slots read so far, so the weights may be compacted in place.
-constexpr int kSelThreads = 1024;
+// k_select: one block per (sequence, head).  The weights of the middle tokens are mapped to unsigned keys of the same order, kept in shared memory (beyond
+// kSelKeys tokens they are read again each time).  The m-th largest key is found 11, 11 and 10 bits at a time by a histogram and a scan of
+// it from the top.  (Two bits at a time, by counting the keys at or above three candidates, needs 16 rounds of a barrier each: 600 keys took 12.5 us, now 9.)  Then each
+// warp counts, and after a scan over the warps writes down, the kept slots of its stretch in order: all keys above the found one, the first of those
+// equal to it.
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kSelKeys = 40960;
 
 __device__ __forceinline__ unsigned weight_key(float w) {
     if (w != w) return 0u;                                   // NaN: below every number
@@ -167,128 +172,194 @@ __device__ __forceinline__ unsigned weight_key(float w) {
 }
 
 __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
-    __shared__ unsigned hist[256];
-    __shared__ unsigned s_prefix, s_left;
-    __shared__ int warp_sum[2][32], base[2];
+    extern __shared__ unsigned s_key[];
+    __shared__ unsigned hist[2048];
+    __shared__ unsigned warp_total[kSelWarps], s_bin, s_left;
+    __shared__ unsigned warp_above[kSelWarps], warp_equal[kSelWarps];
     grid_go();
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int n = kv_length(a.batch, b, true);
     const int64_t row = (int64_t)b * a.heads + h;
-    const float* w = a.w_in + row * a.w_stride;
-    float* wo = a.w_out + row * a.w_stride;
     int* kept = a.kept + row * a.keep;
-    const bool all = n <= a.keep;
-    const int lo = min(a.first, n), hi = max(lo, n - a.recent);
-    unsigned prefix = 0, left = all ? 0 : (unsigned)(a.keep - a.first - a.recent);      // (first + recent <= keep < n)
-    if (!all) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
-            __syncthreads();
-            for (int i = lo + tid; i < hi; i += kSelThreads) {
-                const unsigned k = weight_key(w[i]);
-                if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
-            }
-            __syncthreads();
-            if (tid < 32) {                                  // bins from the top: lane l holds bins 255 - 8 l ... 248 - 8 l
-                unsigned c[8], sum = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { c[j] = hist[255 - 8 * lane - j]; sum += c[j]; }
-                unsigned before = sum;
-                for (int o = 1; o < 32; o <<= 1) { const unsigned v = __shfl_up_sync(~0u, before, o); if (lane >= o) before += v; }
-                before -= sum;
-                // the bin in which the `left` largest end (left 0: none is taken, any bin that holds nothing above it)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (before <= left && left < before + c[j]) { s_prefix = prefix | ((unsigned)(255 - 8 * lane - j) << shift); s_left = left - before; }
-                    before += c[j];
-                }
-            }
-            __syncthreads();
-            prefix = s_prefix; left = s_left;
-            __syncthreads();
-        }
+    if (n <= a.keep) {
+        for (int i = tid; i < a.keep; i += kSelThreads) kept[i] = i < n ? i : -1;
+        return;
     }
-    // keys above `prefix` are kept, and the first `left` of those equal to it
-    if (tid < 2) base[tid] = 0;
+    const int lo = a.first, hi = n - a.recent, len = hi - lo;            // (first + recent <= keep < n)
+    const unsigned left = (unsigned)(a.keep - a.first - a.recent);       // < len
+    const float* w = a.w_in + row * a.w_stride + lo;
+    const bool held = len <= kSelKeys;
+    if (held) for (int i = tid; i < len; i += kSelThreads) s_key[i] = weight_key(w[i]);
     __syncthreads();
-    for (int i0 = 0; i0 < n; i0 += kSelThreads) {
-        const int i = i0 + tid;
-        float v = 0.f;
-        bool keep = false, equal = false;
-        if (i < n) {
-            v = w[i];
-            if (all || i < lo || i >= hi) keep = true;
-            else {
-                const unsigned k = weight_key(v);
-                keep = k > prefix; equal = k == prefix;
-            }
-        }
-        const unsigned be = __ballot_sync(~0u, equal);
-        if (lane == 0) warp_sum[0][warp] = __popc(be);
+    auto key = [&](int i) { return held ? s_key[i] : weight_key(w[i]); };
+    unsigned found = 0, want = left;
+    if (left == 0) found = 0xffffffffu;                                  // (above every key)
+    for (int pass = 0; pass < 3 && left > 0; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const unsigned mask = pass == 2 ? 1023u : 2047u;
+        for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
         __syncthreads();
-        int before = base[0];
-        for (int j = 0; j < warp; ++j) before += warp_sum[0][j];
-        if (equal && (unsigned)(before + __popc(be & ((1u << lane) - 1))) < left) keep = true;
-        const unsigned bk = __ballot_sync(~0u, keep);
-        if (lane == 0) warp_sum[1][warp] = __popc(bk);
-        __syncthreads();
-        int at = base[1];
-        for (int j = 0; j < warp; ++j) at += warp_sum[1][j];
-        at += __popc(bk & ((1u << lane) - 1));
-        if (keep) { kept[at] = i; wo[at] = v; }
-        __syncthreads();
-        if (tid == kSelThreads - 1) {
-            base[1] = at + (keep ? 1 : 0);
-            base[0] = before + __popc(be);
+#pragma unroll 4
+        for (int i = tid; i < len; i += kSelThreads) {
+            const unsigned k = key(i);
+            if (pass == 0 || (k >> (pass == 1 ? 21 : 10)) == (found >> (pass == 1 ? 21 : 10))) atomicAdd(&hist[(k >> shift) & mask], 1u);
         }
         __syncthreads();
+        // bins from the top, 4 a thread: the one in which the want-th largest lies
+        unsigned c[4], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += c[j] = hist[2047 - 4 * tid - j];
+        unsigned upto = sum;
+        for (int o = 1; o < 32; o <<= 1) { const unsigned v = __shfl_up_sync(~0u, upto, o); if (lane >= o) upto += v; }
+        if (lane == 31) warp_total[warp] = upto;
+        __syncthreads();
+        for (int j = 0; j < warp; ++j) upto += warp_total[j];
+        unsigned before = upto - sum;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (before < want && want <= before + c[j]) { s_bin = 2047 - 4 * tid - j; s_left = want - before; }
+            before += c[j];
+        }
+        __syncthreads();
+        found |= s_bin << shift;
+        want = s_left;
     }
-    const int total = all ? n : a.keep;
-    for (int i = total + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
-    for (int i = total + tid; i < n; i += kSelThreads) wo[i] = 0.f;
+    const int stretch = (len + kSelThreads - 1) / kSelThreads * 32, i0 = warp * stretch, i1 = min(len, i0 + stretch);
+    unsigned above = 0, equal = 0;
+    for (int i = i0; i < i1; i += 32) {
+        const unsigned k = i + lane < i1 ? key(i + lane) : 0u;
+        above += __popc(__ballot_sync(~0u, i + lane < i1 && k > found));
+        equal += __popc(__ballot_sync(~0u, i + lane < i1 && k == found));
+    }
+    if (lane == 0) { warp_above[warp] = above; warp_equal[warp] = equal; }
+    __syncthreads();
+    unsigned all_above = 0, above_before = 0, equal_before = 0;
+    for (int j = 0; j < kSelWarps; ++j) {
+        all_above += warp_above[j];
+        if (j < warp) { above_before += warp_above[j]; equal_before += warp_equal[j]; }
+    }
+    const unsigned take = left - all_above;                              // of the equal ones
+    for (int i = i0; i < i1; i += 32) {
+        const bool in = i + lane < i1;
+        const unsigned k = in ? key(i + lane) : 0u, below = (1u << lane) - 1;
+        const unsigned ba = __ballot_sync(~0u, in && k > found), be = __ballot_sync(~0u, in && k == found);
+        const unsigned at_above = above_before + __popc(ba & below), at_equal = equal_before + __popc(be & below);
+        if (in && (k > found || (k == found && at_equal < take))) kept[lo + at_above + min(at_equal, take)] = lo + i + lane;
+        above_before += __popc(ba);
+        equal_before += __popc(be);
+    }
+    for (int i = tid; i < lo; i += kSelThreads) kept[i] = i;
+    for (int i = tid; i < a.recent; i += kSelThreads) kept[a.keep - a.recent + i] = hi + i;
 }
 
-// k_move: one block per (sequence, head, 64-byte slice of the key or the value rows): slices of a row move independently, so in place they are in nobody's
-// way.  A wave of rows is read, the block waits, and the wave is written: row r comes from slot kept[r] >= r, so later waves read nothing that was written.
-constexpr int kMoveThreads = 256, kMoveDepth = 8;
+// k_move: moves the kept rows, a few blocks for the key and the value rows of each (sequence, head).  To other pages: every block takes a range of rows, whole rows at a
+// time.  In place: every block takes a slice of 64 bytes of all rows, since slices move independently; a wave of rows is read, the block waits,
+// and the wave is written.  Row r comes from slot kept[r] >= r, so later waves read nothing that was written.  Three waves are under way at
+// once in both: the slots of the next but one, the pages of the next, the rows of this.  One more block a head moves the weights, in waves as well.
+constexpr int kMoveThreads = 256, kMoveDepth = 4;
 
-__global__ void __launch_bounds__(kMoveThreads) k_move(const EvictArgs a) {
-    grid_wait();
-    const int h = blockIdx.y, b = blockIdx.z, slices = a.head_dim / 32;
-    const bool val = (int)blockIdx.x >= slices;
-    const int slice = blockIdx.x - (val ? slices : 0);
+template <int LANES, bool IN_PLACE>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, uint16_t* pool, int64_t page_s, int64_t token_s, const int* kept, const int* from, const int* to, int r0, int room) {
+    constexpr int kRows = kMoveThreads / LANES, kWave = kMoveDepth * kRows;
     const Batch& B = a.batch;
-    const int count = min(kv_length(B, b, false), a.keep);
-    const int64_t page_s = val ? a.v_page : a.k_page, token_s = val ? a.v_token : a.k_token, head_s = val ? a.v_head : a.k_head;
-    uint16_t* pool = (uint16_t*)(val ? a.v_pool : a.k_pool) + h * head_s + slice * 32 + (threadIdx.x & 3) * 8;
+    const int mine = (int)threadIdx.x / LANES;
+    pool += threadIdx.x % LANES * 8;
+    int slot[2][kMoveDepth], pf[kMoveDepth], pt[kMoveDepth];
+    auto slots = [&](int r0, int (&s)[kMoveDepth]) {
+#pragma unroll
+        for (int u = 0; u < kMoveDepth; ++u) {
+            const int r = r0 + u * kRows + mine;
+            s[u] = r < room ? kept[r] : -1;
+        }
+    };
+    auto pages = [&](int r0, const int (&s)[kMoveDepth]) {
+#pragma unroll
+        for (int u = 0; u < kMoveDepth; ++u) {
+            const int r = r0 + u * kRows + mine;
+            pf[u] = s[u] >= 0 ? from[s[u] / B.page_size] : 0;
+            pt[u] = s[u] >= 0 ? to[r / B.page_size] : 0;
+        }
+    };
+    slots(r0, slot[0]);
+    slots(r0 + kWave, slot[1]);
+    pages(r0, slot[0]);
+    for (; r0 < room; r0 += kWave) {
+        int64_t dst[kMoveDepth];
+        uint4 v[kMoveDepth];
+        bool bad = false;
+#pragma unroll
+        for (int u = 0; u < kMoveDepth; ++u) {
+            const int r = r0 + u * kRows + mine, s = slot[0][u];
+            const int64_t src = pf[u] * page_s + (s % B.page_size) * token_s;
+            dst[u] = pt[u] * page_s + (r % B.page_size) * token_s;
+            const bool off = pf[u] < 0 || pf[u] >= B.num_pages || pt[u] < 0 || pt[u] >= B.num_pages;
+            bad |= off;
+            if (s < 0 || off || src == dst[u]) dst[u] = -1;
+            if (dst[u] >= 0) v[u] = *(const uint4*)(pool + src);
+            slot[0][u] = slot[1][u];
+        }
+        slots(r0 + 2 * kWave, slot[1]);
+        pages(r0 + kWave, slot[0]);
+        if (bad) atomicOr(B.status, kBadPage);
+        if (IN_PLACE) __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kMoveDepth; ++u)
+            if (dst[u] >= 0) *(uint4*)(pool + dst[u]) = v[u];
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) k_move(const EvictArgs a, const int shares, const bool write_len) {
+    const int h = blockIdx.y, b = blockIdx.z;
+    grid_wait();
+    const Batch& B = a.batch;
+    const int n = kv_length(B, b, false), count = min(n, a.keep);
     const int* kept = a.kept + ((int64_t)b * a.heads + h) * a.keep;
+    if ((int)blockIdx.x == 2 * shares) {
+        if (write_len && h == 0 && threadIdx.x == 0) a.new_len[b] = count;
+        const float* w = a.w_in + ((int64_t)b * a.heads + h) * a.w_stride;
+        float* out = a.w_out + ((int64_t)b * a.heads + h) * a.w_stride;
+        for (int r0 = 0; r0 < n; r0 += kMoveDepth * kMoveThreads) {
+            float v[kMoveDepth];
+#pragma unroll
+            for (int u = 0; u < kMoveDepth; ++u) {
+                const int r = r0 + u * kMoveThreads + threadIdx.x;
+                v[u] = r < count ? w[kept[r]] : 0.f;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kMoveDepth; ++u) {
+                const int r = r0 + u * kMoveThreads + threadIdx.x;
+                if (r < n) out[r] = v[u];
+            }
+        }
+        return;
+    }
+    const bool val = (int)blockIdx.x >= shares;
+    const int share = blockIdx.x - (val ? shares : 0);
+    const int64_t page_s = val ? a.v_page : a.k_page, token_s = val ? a.v_token : a.k_token;
+    uint16_t* pool = (uint16_t*)(val ? a.v_pool : a.k_pool) + h * (val ? a.v_head : a.k_head);
     const int* from = B.table + b * B.table_stride;
     const int* to = a.new_table + b * a.new_table_stride;
     const int room = (int)min((int64_t)a.new_max_pages * B.page_size, (int64_t)count);
     if (room < count && threadIdx.x == 0) atomicOr(B.status, kBadLength);
-    for (int r0 = 0; r0 < room; r0 += kMoveDepth * (kMoveThreads / 4)) {
-        uint4 v[kMoveDepth];
-        int64_t at[kMoveDepth];
-#pragma unroll
-        for (int u = 0; u < kMoveDepth; ++u) {
-            const int r = r0 + u * (kMoveThreads / 4) + (threadIdx.x >> 2);
-            at[u] = -1;
-            if (r < room) {
-                const int s = kept[r];
-                const int pf = from[s / B.page_size], pt = to[r / B.page_size];
-                if (pf < 0 || pf >= B.num_pages || pt < 0 || pt >= B.num_pages) atomicOr(B.status, kBadPage);
-                else if (pf != pt || s % B.page_size != r % B.page_size) {
-                    v[u] = *(const uint4*)(pool + pf * page_s + (s % B.page_size) * token_s);
-                    at[u] = pt * page_s + (r % B.page_size) * token_s;
-                }
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kMoveDepth; ++u)
-            if (at[u] >= 0) *(uint4*)(pool + at[u]) = v[u];
+    // in place: the two tables agree somewhere (where one does not end before the other)
+    const int both = min((room + B.page_size - 1) / B.page_size, B.max_pages);
+    bool agree = false;
+    for (int i = threadIdx.x; i < both; i += kMoveThreads) agree |= from[i] == to[i];
+    if (__syncthreads_or(agree)) {
+        if (share < D / 32) move_rows<4, true>(a, pool + share * 32, page_s, token_s, kept, from, to, 0, room);
+    } else {
+        const int per = (room + shares - 1) / shares;
+        move_rows<D / 8, false>(a, pool, page_s, token_s, kept, from, to, share * per, min(room, (share + 1) * per));
     }
-    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) a.new_len[b] = count;
+}
+
+// New lengths written over the old ones: only once every block that reads the old ones is done.
+__global__ void k_new_len(const EvictArgs a) {
+    grid_wait();
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b < a.batch.batch) a.new_len[b] = min(kv_length(a.batch, b, false), a.keep);
 }
 
 }  // namespace
@@ -302,12 +373,22 @@ cudaError_t launch_rows(const RowsArgs& a, int dtype, int sm_count, cudaStream_t
 }
 
 cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream) {
-    k_select<<<dim3(a.heads, a.batch.batch), kSelThreads, 0, stream>>>(a);
-    ++g_launches;
-    cudaError_t e = cudaGetLastError();
+    const size_t smem = sizeof(unsigned) * (size_t)(a.batch.max_len < kSelKeys ? a.batch.max_len : kSelKeys);
+    cudaError_t e = cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeys * sizeof(unsigned));
     if (e != cudaSuccess) return e;
+    k_select<<<dim3(a.heads, a.batch.batch), kSelThreads, smem, stream>>>(a);
     ++g_launches;
-    return launch_behind(stream, dim3(2 * a.head_dim / 32, a.heads, a.batch.batch), dim3(kMoveThreads), 0, k_move, a);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    const bool over = a.new_len < a.batch.kv_len + a.batch.batch && a.batch.kv_len < a.new_len + a.batch.batch;
+    // blocks for about 16 KB in flight on every SM twice over, of 64 rows or more; in place as many as a row has slices of 64 bytes do work
+    int shares = a.head_dim / 32;
+    while (shares < 32 && 2 * (int64_t)shares * a.heads * a.batch.batch < 1200 && a.keep / (2 * shares) >= 64) shares *= 2;
+    const dim3 grid(2 * shares + 1, a.heads, a.batch.batch);
+    ++g_launches;
+    e = launch_behind(stream, grid, dim3(kMoveThreads), 0, a.head_dim == 128 ? k_move<128> : k_move<64>, a, shares, !over);
+    if (e != cudaSuccess || !over) return e;
+    ++g_launches;
+    return launch_behind(stream, dim3((unsigned)ceil_div(a.batch.batch, 256)), dim3(256), 0, k_new_len, a);
 }
 
 }  // namespace kv
