@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_int32, c_int64, c_size_t, c_void_p
 
@@ -134,17 +135,18 @@ def _load() -> ctypes.CDLL:
     lib.fd_unit_peaks.argtypes = [c_void_p, c_size_t, c_void_p, POINTER(fd_unit_rates)]
     lib.fd_unit_peaks.restype = c_int32
     lib.fd_rotary_frequencies.argtypes = [c_int32, c_double, c_int32, c_double, c_double, c_double, c_double, POINTER(c_double)]
-    lib.fd_rotary.argtypes = [POINTER(fd_heads), POINTER(fd_heads), c_int32, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_int32,
+    # (structures of arguments come as pointers or as packed bytes: see _HEADS)
+    lib.fd_rotary.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_int32,
                               c_double, c_int32, c_void_p, c_char_p, c_size_t]
     lib.fd_kv_create.argtypes = [POINTER(c_void_p), POINTER(fd_kv_desc), c_char_p, c_size_t]
     lib.fd_kv_destroy.argtypes = [c_void_p]
     lib.fd_kv_destroy.restype = None
     lib.fd_kv_synchronize.argtypes = [c_void_p, c_void_p]
-    lib.fd_kv_append.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_append_args), c_void_p, c_char_p, c_size_t]
+    lib.fd_kv_append.argtypes = [c_void_p, POINTER(fd_kv_batch), c_void_p, c_void_p, c_char_p, c_size_t]
     lib.fd_kv_attend_bytes.argtypes = [c_void_p, POINTER(fd_kv_batch), c_int32, c_int32]
     lib.fd_kv_attend_bytes.restype = c_size_t
-    lib.fd_kv_attend.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_attend_args), c_void_p, c_size_t, c_void_p, c_char_p, c_size_t]
-    lib.fd_kv_evict.argtypes = [c_void_p, POINTER(fd_kv_batch), POINTER(fd_kv_evict_args), c_void_p, c_char_p, c_size_t]
+    lib.fd_kv_attend.argtypes = [c_void_p, POINTER(fd_kv_batch), c_void_p, c_void_p, c_size_t, c_void_p, c_char_p, c_size_t]
+    lib.fd_kv_evict.argtypes = [c_void_p, POINTER(fd_kv_batch), c_void_p, c_void_p, c_char_p, c_size_t]
     for name in ("fd_rotary_frequencies", "fd_rotary", "fd_kv_create", "fd_kv_synchronize", "fd_kv_append", "fd_kv_attend", "fd_kv_evict"):
         getattr(lib, name).restype = c_int32
     lib.fd_status_string.argtypes = [c_int32]
@@ -435,21 +437,30 @@ def _need(cond, what: str):
         _refuse(what)
 
 
-# (These checks and the calls below run once per operator and decoding step, some in less time than the kernel they launch: texts are made where a check fails.)
-def _need_tensor(t, dtype, dims: int, device, what: str):
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != dims or t.device != device:
-        _refuse(f"{what}: a {dims}-d {dtype} tensor on {device}")
+# These checks and the calls below run once per operator and decoding step, some in less time than the kernel they launch.  So texts are made where a check
+# fails, and the structures of fd.h are packed in one step (fd_heads, fd_kv_append_args, fd_kv_attend_args, fd_kv_evict_args; the test-suite holds the
+# formats against the ctypes structures of the same names).
+_HEADS = struct.Struct("@Pqqi4x")
+_APPEND = struct.Struct("@" + "Pqqi4x" * 4 + "PPdii")
+_ATTEND = struct.Struct("@" + "Pqqi4x" * 2 + "diiPPPq")
+_EVICT = struct.Struct("@PPqPqiiiiPP")
+_NO_HEADS = (0, 0, 0, 0)
 
 
-def _heads(t: torch.Tensor, dtype, device, head_dim: int, tokens: int, what: str) -> fd_heads:
-    """[tokens, heads, head_dim] with unit stride inside a head; strides of single tokens and heads do not matter."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 3 or t.device != device:
-        _refuse(f"{what}: a 3-d {dtype} tensor on {device}")
+def _need_tensor(t, dtype, dims: int, index: int, what: str):
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != dims or t.get_device() != index:
+        _refuse(f"{what}: a {dims}-d {dtype} tensor on cuda:{index}")
+
+
+def _heads(t: torch.Tensor, dtype, index: int, head_dim: int, tokens: int, what: str):
+    """[tokens, heads, head_dim] with unit stride inside a head, as the fields of an fd_heads; strides of single tokens and heads do not matter."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 3 or t.get_device() != index:
+        _refuse(f"{what}: a 3-d {dtype} tensor on cuda:{index}")
     n, h, d = t.shape
     st, sh, sd = t.stride()
     if n != tokens or d != head_dim or (sd != 1 and d != 1):
         _refuse(f"{what}: [{tokens}, heads, {head_dim}] with unit stride inside a head")
-    return fd_heads(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d, h)
+    return t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d, h
 
 
 class _Messages(threading.local):
@@ -460,14 +471,14 @@ class _Messages(threading.local):
 _messages = _Messages()
 
 
-def _call(device, fn, *args):
-    """fn(*args, current stream, errbuf, its length) on `device`."""
+def _call(index: int, fn, *args):
+    """fn(*args, current stream, errbuf, its length) on a device."""
     err = _messages.buf
-    if torch._C._cuda_getDevice() == device.index:
-        st = fn(*args, torch._C._cuda_getCurrentRawStream(device.index), err, 256)
+    if torch._C._cuda_getDevice() == index:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(index), err, 256)
     else:
-        with torch.cuda.device(device):
-            st = fn(*args, torch._C._cuda_getCurrentRawStream(device.index), err, 256)
+        with torch.cuda.device(index):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(index), err, 256)
     if st != FD_OK:
         raise FdError(st, err.value.decode())
 
@@ -483,12 +494,13 @@ def fd_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "n
     return torch.tensor(list(out), dtype=torch.float64, device=device)
 
 
-def _rotary_args(positions, freqs, tokens: int, device, layout: str):
-    _need_tensor(positions, torch.int32, 1, device, "positions")
-    _need_tensor(freqs, torch.float64, 1, device, "freqs")
-    if positions.shape[0] != tokens or not positions.is_contiguous():
+def _rotary_args(positions, freqs, tokens: int, index: int, layout: str):
+    _need_tensor(positions, torch.int32, 1, index, "positions")
+    _need_tensor(freqs, torch.float64, 1, index, "freqs")
+    if positions.numel() != tokens or not positions.is_contiguous():
         _refuse(f"positions: {tokens} contiguous values")
-    _need(freqs.is_contiguous(), "freqs must be contiguous")
+    if not freqs.is_contiguous():
+        _refuse("freqs must be contiguous")
     code = _LAYOUTS.get(layout)
     return code if code is not None else _refuse(f"layout: one of {sorted(_LAYOUTS)}")
 
@@ -497,13 +509,16 @@ def fd_rotary(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, lay
               inverse: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotary positions of x [tokens, heads, head_dim] on the current stream; with `inverse` the transpose, which takes the gradient of the
     result to the gradient of x.  `out` may be x."""
-    _need(isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 3 and x.dtype in _DTYPES, "x: a CUDA tensor [tokens, heads, head_dim] of bf16, fp16 or fp32")
+    dt = x.dtype if isinstance(x, torch.Tensor) else None
+    code = _DTYPES.get(dt)
+    if code is None or not x.is_cuda or x.dim() != 3:
+        _refuse("x: a CUDA tensor [tokens, heads, head_dim] of bf16, fp16 or fp32")
+    index = x.get_device()
     tokens, _, d = x.shape
-    code = _rotary_args(positions, freqs, tokens, x.device, layout)
+    order = _rotary_args(positions, freqs, tokens, index, layout)
     y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
-    hx, hy = _heads(x, x.dtype, x.device, d, tokens, "x"), _heads(y, x.dtype, x.device, d, tokens, "out")
-    _call(x.device, lib.fd_rotary, byref(hx), byref(hy), _DTYPES[x.dtype], tokens, d, positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0],
-          code, scale, 1 if inverse else 0)
+    _call(index, lib.fd_rotary, _HEADS.pack(*_heads(x, dt, index, d, tokens, "x")), _HEADS.pack(*_heads(y, dt, index, d, tokens, "out")), code, tokens, d,
+          positions.data_ptr(), freqs.data_ptr(), 2 * freqs.numel(), order, scale, 1 if inverse else 0)
     return y
 
 
@@ -515,9 +530,9 @@ class KVBatch:
     def __init__(self, page_table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor, total_q: int, max_new: int, max_len: int):
         dev = page_table.device
         _need(page_table.is_cuda, "page_table: a CUDA tensor")
-        _need_tensor(page_table, torch.int32, 2, dev, "page_table")
-        _need_tensor(kv_len, torch.int32, 1, dev, "kv_len")
-        _need_tensor(q_start, torch.int32, 1, dev, "q_start")
+        _need_tensor(page_table, torch.int32, 2, dev.index, "page_table")
+        _need_tensor(kv_len, torch.int32, 1, dev.index, "kv_len")
+        _need_tensor(q_start, torch.int32, 1, dev.index, "q_start")
         n = page_table.shape[0]
         _need(page_table.stride(1) == 1 or page_table.shape[1] == 1, "page_table: unit stride inside a row")
         _need(kv_len.shape[0] == n and q_start.shape[0] == n + 1 and kv_len.is_contiguous() and q_start.is_contiguous(),
@@ -539,7 +554,7 @@ class KVCache:
         _need(isinstance(k_pages, torch.Tensor) and k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in (torch.bfloat16, torch.float16),
               "k_pages: a CUDA tensor [page, token, head, head_dim] of bf16 or fp16")
         dev = k_pages.device
-        _need_tensor(v_pages, k_pages.dtype, 4, dev, "v_pages")
+        _need_tensor(v_pages, k_pages.dtype, 4, dev.index, "v_pages")
         _need(k_pages.shape == v_pages.shape and k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "k_pages, v_pages: equal shapes, unit stride inside a head")
         self.device, self.dtype = dev, k_pages.dtype
         self.k_pages, self.v_pages = k_pages, v_pages
@@ -583,17 +598,18 @@ class KVCache:
     def append(self, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor | None = None, freqs: torch.Tensor | None = None,
                layout: str = "half", scale: float = 1.0, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
         """Writes the new tokens' keys (rotated, if there are positions) and values into the cache; rotates q beside them and returns it."""
-        n, dev, dt, d = batch.total_q, self.device, self.dtype, self.head_dim
-        a = fd_kv_append_args(_heads(k, dt, dev, d, n, "k"), _heads(v, dt, dev, d, n, "v"))
+        n, index, dt, d = batch.total_q, self.device.index, self.dtype, self.head_dim
+        ref = self._batch(batch)
+        rot, hq, ho = (0, 0, scale, 0, 0), _NO_HEADS, _NO_HEADS
         if positions is not None:
-            a.layout = _rotary_args(positions, freqs, n, dev, layout)
-            a.positions_dev, a.freqs_dev, a.rot_dim = positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0]
-        a.scale = scale
+            order = _rotary_args(positions, freqs, n, index, layout)
+            rot = (positions.data_ptr(), freqs.data_ptr(), scale, 2 * freqs.numel(), order)
         if q is not None:
-            a.q = _heads(q, dt, dev, d, n, "q")
-            q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
-            a.q_out = _heads(q_out, dt, dev, d, n, "q_out")
-        _call(dev, lib.fd_kv_append, self._h, self._batch(batch), byref(a))
+            hq = _heads(q, dt, index, d, n, "q")
+            if q_out is None:
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            ho = _heads(q_out, dt, index, d, n, "q_out")
+        _call(index, lib.fd_kv_append, self._h, ref, _APPEND.pack(*_heads(k, dt, index, d, n, "k"), *_heads(v, dt, index, d, n, "v"), *hq, *ho, *rot))
         return q_out
 
     def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, causal: bool = True, window: int = 0,
@@ -602,61 +618,70 @@ class KVCache:
         """Returns (out, lse) for the new tokens' queries [total_q, query heads, head_dim]; scale defaults to head_dim^-1/2.  With `weights`
         ([batch, heads, >= max_len] fp32) and / or `weights_out` (default: weights itself) the softmax weights that every cached token received are
         added up: weights_out = weights (or 0) + their sum."""
-        n, dev, dt, d = batch.total_q, self.device, self.dtype, self.head_dim
-        hq = _heads(q, dt, dev, d, n, "q")
+        n, index, dt, d = batch.total_q, self.device.index, self.dtype, self.head_dim
+        ref = self._batch(batch)
+        hq = _heads(q, dt, index, d, n, "q")
+        heads = hq[3]
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if lse is None:
-            lse = torch.empty((n, hq.heads), dtype=torch.float32, device=dev)
+            lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
         else:
-            _need_tensor(lse, torch.float32, 2, dev, "lse")
-            _need(lse.shape == q.shape[:2] and lse.is_contiguous(), "lse: [total_q, query heads], contiguous")
-        a = fd_kv_attend_args(hq, _heads(out, dt, dev, d, n, "out"), d ** -0.5 if scale is None else scale, 1 if causal else 0, window or 0, lse.data_ptr())
+            _need_tensor(lse, torch.float32, 2, index, "lse")
+            if lse.shape != (n, heads) or not lse.is_contiguous():
+                _refuse("lse: [total_q, query heads], contiguous")
+        w_in = w_out = w_stride = 0
         if weights is not None or weights_out is not None:
-            weights_out = weights if weights_out is None else weights_out
-            for t in (weights, weights_out):
-                if t is not None:
-                    self._check_weights(t, batch)
-                    _need(t.stride() == weights_out.stride(), "weights and weights_out: equal strides")
-            a.weights_in_dev, a.weights_out_dev = _ptr(weights), weights_out.data_ptr()
-            a.weights_stride = weights_out.stride(1)
-        b = self._batch(batch)
-        size = lib.fd_kv_attend_bytes(self._h, b, hq.heads, 1 if weights_out is not None else 0)
-        ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
-        _call(dev, lib.fd_kv_attend, self._h, b, byref(a), _ptr(ws), size)
+            if weights_out is None:
+                weights_out = weights
+            w_stride = self._check_weights(weights_out, batch)
+            w_out = weights_out.data_ptr()
+            if weights is not None:
+                if self._check_weights(weights, batch) != w_stride:
+                    _refuse("weights and weights_out: equal shapes")
+                w_in = weights.data_ptr()
+        size = lib.fd_kv_attend_bytes(self._h, ref, heads, 1 if w_out else 0)
+        ws = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
+        _call(index, lib.fd_kv_attend, self._h, ref, _ATTEND.pack(*hq, *_heads(out, dt, index, d, n, "out"), d ** -0.5 if scale is None else scale,
+                                                                 1 if causal else 0, window or 0, lse.data_ptr(), w_in, w_out, w_stride),
+              None if ws is None else ws.data_ptr(), size)
         return out, lse
 
-    def _check_weights(self, t: torch.Tensor, batch: KVBatch):
-        _need_tensor(t, torch.float32, 3, self.device, "weights")
+    def _check_weights(self, t: torch.Tensor, batch: KVBatch) -> int:
+        _need_tensor(t, torch.float32, 3, self.device.index, "weights")
         n, h, length = t.shape
         if n != batch.batch or h != self.heads or length < batch.max_len or not t.is_contiguous():
             _refuse(f"weights: [{batch.batch}, {self.heads}, {batch.max_len} or more], contiguous")
+        return length
 
     def evict(self, batch: KVBatch, weights: torch.Tensor, keep: int, first: int = 0, recent: int = 0, new_table: torch.Tensor | None = None,
               kept: torch.Tensor | None = None, new_len: torch.Tensor | None = None, weights_out: torch.Tensor | None = None):
         """Every head keeps `keep` tokens of each longer sequence: the first, the recent and the heaviest of the others, in order, moved to
         the front of the sequence's pages (or to new_table's).  Returns (kept slots [batch, heads, keep], new lengths, weights)."""
-        dev = self.device
-        self._check_weights(weights, batch)
-        weights_out = weights if weights_out is None else weights_out
-        self._check_weights(weights_out, batch)
-        _need(weights_out.stride() == weights.stride(), "weights and weights_out: equal strides")
+        index, ref = self.device.index, self._batch(batch)
+        w_stride = self._check_weights(weights, batch)
+        if weights_out is None:
+            weights_out = weights
+        elif self._check_weights(weights_out, batch) != w_stride:
+            _refuse("weights and weights_out: equal shapes")
         table = batch.page_table if new_table is None else new_table
-        _need_tensor(table, torch.int32, 2, dev, "new_table")
-        _need(table.shape[0] == batch.batch and (table.stride(1) == 1 or table.shape[1] == 1), "new_table: [batch, pages], unit stride inside a row")
+        _need_tensor(table, torch.int32, 2, index, "new_table")
+        rows, cols = table.shape
+        row, unit = table.stride()
+        if rows != batch.batch or (unit != 1 and cols != 1):
+            _refuse("new_table: [batch, pages], unit stride inside a row")
         if kept is None:
-            kept = torch.empty((batch.batch, self.heads, max(keep, 0)), dtype=torch.int32, device=dev)
+            kept = torch.empty((batch.batch, self.heads, max(keep, 0)), dtype=torch.int32, device=self.device)
         if new_len is None:
-            new_len = torch.empty(batch.batch, dtype=torch.int32, device=dev)
-        _need_tensor(kept, torch.int32, 3, dev, "kept")
-        _need_tensor(new_len, torch.int32, 1, dev, "new_len")
+            new_len = torch.empty(batch.batch, dtype=torch.int32, device=self.device)
+        _need_tensor(kept, torch.int32, 3, index, "kept")
+        _need_tensor(new_len, torch.int32, 1, index, "new_len")
         if kept.shape != (batch.batch, self.heads, keep) or not kept.is_contiguous():
             _refuse(f"kept: [{batch.batch}, {self.heads}, {keep}], contiguous")
-        if new_len.shape[0] != batch.batch or not new_len.is_contiguous():
+        if new_len.numel() != batch.batch or not new_len.is_contiguous():
             _refuse(f"new_len: {batch.batch} contiguous values")
-        a = fd_kv_evict_args(weights.data_ptr(), weights_out.data_ptr(), weights.stride(1), table.data_ptr(), max(table.stride(0), table.shape[1]),
-                             table.shape[1], keep, first, recent, kept.data_ptr(), new_len.data_ptr())
-        _call(dev, lib.fd_kv_evict, self._h, self._batch(batch), byref(a))
+        _call(index, lib.fd_kv_evict, self._h, ref, _EVICT.pack(weights.data_ptr(), weights_out.data_ptr(), w_stride, table.data_ptr(), max(row, cols), cols,
+                                                                keep, first, recent, kept.data_ptr(), new_len.data_ptr()))
         return kept, new_len, weights_out
 
 

@@ -25,7 +25,6 @@ namespace {
 using namespace tc;
 
 constexpr int kSoftWarps = 8, kThreadsAt = 32 * (kSoftWarps + 4);
-constexpr int kWeighWarps = 16, kThreadsWe = 32 * (kWeighWarps + 3);
 constexpr int kPolyEvery = 0;            // every so many pairs of exponentials are taken on the FMA pipe; 0: none
 
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
@@ -454,56 +453,62 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     }
 }
 
-// k_weigh: what every cached token received, w_j += sum over rows of 2^(c s - lse).  One CTA takes two tiles of 128 cached tokens as the M side (S^T = K Q^T: a
-// thread owns a token, so the sum over rows is a sum over its columns and needs no exchange) and goes through the rows that see them.
-constexpr int kWeighSlots = 3, kWeighPoly = 0;
+// k_weigh: what every cached token received, w_j += sum over rows of 2^(c s - lse).  One CTA takes a tile of 128 cached tokens as the M side (S^T = K Q^T: a thread
+// owns a token, so the sum over rows is a sum over its columns and needs no exchange) and goes through the rows that see them, 128 at a
+// time; two warpgroups share the columns.  The exponentials bound it.  Two CTAs an SM fill each other's waits and even out the lengths: with
+// one CTA of two tiles 2 x 2048 new tokens over 8192 and 4900 took 365 us.
+constexpr int kWeighWarps = 8, kThreadsWe = 32 * (kWeighWarps + 3), kWeighCols = 256;
 template <int D>
-struct WeighSmem {
-    static constexpr int kBytes = 1024 + (2 + kWeighSlots) * Geo<D>::kTile + 4 * 128 * 4 + 2 * 128 * 4 + 512;
+struct GeoWeigh {
+    static constexpr int kSlots = D == 128 ? 2 : 4;               // ring of row tiles
+    static constexpr int kSmem = 1024 + (1 + kSlots) * Geo<D>::kTile + 4 * 128 * 4 + 128 * 4 + 512;
 };
+template <int D>
 struct WeighBars {
-    uint64_t k_full, full[kWeighSlots], empty[kWeighSlots], s_full[2][2], s_empty[2][2], l_full[4];
+    uint64_t k_full, full[GeoWeigh<D>::kSlots], empty[GeoWeigh<D>::kSlots], s_full[2], s_empty[2], l_full[4];
     uint32_t tmem_base;
     int abort_flag;
 };
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreadsWe, 1)
+__global__ void __launch_bounds__(kThreadsWe, 2)
 k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const AttendArgs a) {
     using G = Geo<D>;
+    constexpr int kSlots = GeoWeigh<D>::kSlots;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* base = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* k_base = base;
-    uint8_t* ring = base + 2 * G::kTile;
-    float* l_ring = (float*)(ring + kWeighSlots * G::kTile);                  // [4][128]: -lse of a row tile, -inf for rows that are none
-    float* s_acc = l_ring + 4 * 128;                                          // [tile][token]: sums of the second column halves
-    WeighBars* bars = (WeighBars*)(s_acc + 2 * 128);
+    uint8_t* ring = base + G::kTile;
+    float* l_ring = (float*)(ring + kSlots * G::kTile);                       // [4][128]: -lse of a row tile, -inf for rows that are none
+    float* s_acc = l_ring + 4 * 128;                                          // [token]: sums of the second column halves
+    WeighBars<D>* bars = (WeighBars<D>*)(s_acc + 128);
     volatile int* abort_flag = &bars->abort_flag;
     unsigned int* status = a.batch.status + 1;
 
-    const int h = blockIdx.y, b = blockIdx.z, key0 = blockIdx.x * 256;
+    const int h = blockIdx.y, b = blockIdx.z, key0 = blockIdx.x * 128;
     Work w;
     w.b = b; w.begin = q_begin(a.batch, b); w.count = max(0, q_begin(a.batch, b + 1) - w.begin); w.n = kv_length(a.batch, b, false); w.t0 = 0;
     w = uniform(w);
     if (key0 >= w.n) return;
-    const int tiles = w.n - key0 > 128 ? 2 : 1, key_last = min(w.n, key0 + 256) - 1, off = w.n - w.count;
+    const int key_last = min(w.n, key0 + 128) - 1, off = w.n - w.count;
     // tokens that see one of these slots: [ta, tb)
-    const int ta = a.causal ? max(0, key0 - off) : 0, tb = a.window ? min((int64_t)w.count, max((int64_t)0, (int64_t)key_last - off + a.window)) : w.count;
+    const int ta = a.causal ? max(0, key0 - off) : 0, tb = a.window ? (int)min((int64_t)w.count, max((int64_t)0, (int64_t)key_last - off + a.window)) : w.count;
     const int q0 = ta / a.tile_tokens, num = tb > ta ? (tb - 1) / a.tile_tokens + 1 - q0 : 0;
     const int rows = a.tile_tokens * a.group;
 
     const int warp = warp_index(), lane = threadIdx.x & 31;
-    const int key = key0 + ((warp >> 2) & 1) * 128 + (warp & 3) * 32 + lane;          // of the first 16 warps
+    const int key = key0 + (warp & 3) * 32 + lane;                            // of the first 8 warps
     float acc = 0.f;
     if (threadIdx.x == 0) {
         mbar_init(&bars->k_full, 1);
-        for (int s = 0; s < kWeighSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
-        for (int i = 0; i < 4; ++i) { mbar_init(&bars->s_full[i >> 1][i & 1], 1); mbar_init(&bars->s_empty[i >> 1][i & 1], 8); mbar_init(&bars->l_full[i], 1); }
+        for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bars->s_full[i], 1); mbar_init(&bars->s_empty[i], kWeighWarps); }
+        for (int i = 0; i < 4; ++i) mbar_init(&bars->l_full[i], 1);
         bars->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kWeighWarps) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(kWeighCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -513,39 +518,22 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
 
     if (warp == kWeighWarps && num > 0) {
         // -------------------------------------------------------------------- TMA
-        bool ok = true;
-        {   // both key tiles arrive on one barrier: bytes first, then the copies
-            const int boxes = 128 / a.box_rows;
-            int count = 0;
-            for (int t = 0; t < tiles; ++t) count += __popc(__ballot_sync(~0u, lane < boxes && key0 + t * 128 + lane * a.box_rows < w.n));
-            if (lane == 0) mbar_expect_tx(&bars->k_full, count * a.box_rows * D * 2);
-            __syncwarp();
-            for (int t = 0; t < tiles; ++t) {
-                const int key = key0 + t * 128 + lane * a.box_rows;
-                if (lane < boxes && key < w.n) {
-                    int page = a.batch.table[b * a.batch.table_stride + key / a.batch.page_size];
-                    if (page < 0 || page >= a.batch.num_pages) { page = a.batch.num_pages; atomicOr(a.batch.status, kBadPage); }
-#pragma unroll
-                    for (int c = 0; c < G::kChunks; ++c)
-                        tma_load_4d(k_base + t * G::kTile + c * G::kChunkBytes + lane * a.box_rows * 128, &map_k, c * 64, key % a.batch.page_size, h, page, &bars->k_full);
-                }
-            }
-            __syncwarp();
-        }
-        int it = 0;
+        load_tile<D>(k_base, &map_k, a, w, blockIdx.x, h, &bars->k_full);
         if (lane == 0) {
+            bool ok = true;
+            int it = 0;
             for (; it < num && ok; ++it) {
-                const int s = it % kWeighSlots;
-                ok = mbar_wait(&bars->empty[s], ((it / kWeighSlots) & 1) ^ 1, abort_flag, status, 21);
+                const int s = it % kSlots;
+                ok = mbar_wait(&bars->empty[s], ((it / kSlots) & 1) ^ 1, abort_flag, status, 21);
                 if (!ok) break;
                 mbar_expect_tx(&bars->full[s], rows * D * 2);
                 for (int c = 0; c < G::kChunks; ++c)
                     tma_load_3d(ring + s * G::kTile + c * G::kChunkBytes, &map_q, c * 64, h * a.group, w.begin + (q0 + it) * a.tile_tokens, &bars->full[s]);
             }
             if (!ok) {
-                for (int k = max(0, it - kWeighSlots); k < it; ++k) {
+                for (int k = max(0, it - kSlots); k < it; ++k) {
                     const long long c0 = clock64();
-                    while (!mbar_try_wait(&bars->full[k % kWeighSlots], (k / kWeighSlots) & 1) && clock64() - c0 < 20000000ll) {}
+                    while (!mbar_try_wait(&bars->full[k % kSlots], (k / kSlots) & 1) && clock64() - c0 < 20000000ll) {}
                 }
                 const long long c0 = clock64();
                 while (!mbar_try_wait(&bars->k_full, 0) && clock64() - c0 < 20000000ll) {}
@@ -559,42 +547,50 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
             const uint32_t k_lo = (uint32_t)kd, q_lo = (uint32_t)qd, hi = (uint32_t)(kd >> 32);
             bool ok = mbar_wait(&bars->k_full, 0, abort_flag, status, 22);
             for (int i = 0; i < num && ok; ++i) {
-                const int s = i % kWeighSlots, buf = i & 1;
-                ok = mbar_wait(&bars->full[s], (i / kWeighSlots) & 1, abort_flag, status, 23);
-                for (int t = 0; t < tiles && ok; ++t) {
-                    ok = mbar_wait(&bars->s_empty[t][buf], ((i >> 1) & 1) ^ 1, abort_flag, status, 24);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t s_addr = tmem + 256u * t + 128u * buf, kt = k_lo + (uint32_t)(t * G::kTile >> 4), qt = q_lo + (uint32_t)(s * G::kTile >> 4);
+                const int s = i % kSlots, buf = i & 1;
+                ok = mbar_wait_near(&bars->full[s], (i / kSlots) & 1, abort_flag, status, 23) &&
+                     mbar_wait_near(&bars->s_empty[buf], ((i >> 1) & 1) ^ 1, abort_flag, status, 24);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t s_addr = tmem + 128u * buf, qt = q_lo + (uint32_t)(s * G::kTile >> 4);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t o = (uint32_t)((k / 4) * (G::kChunkBytes >> 4) + (k % 4) * 2);
-                        if (k == 0) mma_ss2<0>(s_addr, kt + o, hi, qt + o, hi, id);
-                        else mma_ss2<1>(s_addr, kt + o, hi, qt + o, hi, id);
-                    }
-                    tc_commit(&bars->s_full[t][buf]);
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t o = (uint32_t)((k / 4) * (G::kChunkBytes >> 4) + (k % 4) * 2);
+                    if (k == 0) mma_ss2<0>(s_addr, k_lo + o, hi, qt + o, hi, id);
+                    else mma_ss2<1>(s_addr, k_lo + o, hi, qt + o, hi, id);
                 }
-                if (ok) tc_commit(&bars->empty[s]);
+                tc_commit(&bars->s_full[buf]);
+                tc_commit(&bars->empty[s]);
             }
         }
     } else if (warp == kWeighWarps + 2 && num > 0) {
         // -------------------------------------------------------------------- -lse of each row tile, in powers of two
+        // (This warp has to keep up with a tile of exponentials: places are worked out once, and the next tile's values are under way while this tile's wait.)
+        constexpr float kHi = 1.44269502f, kLo = 1.92596303e-8f;               // log2(e)
+        int token[4], at[4];
+        float next[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = lane + 32 * k;
+            token[k] = r < rows ? q0 * a.tile_tokens + r / a.group : 1 << 30;
+            at[k] = r / a.group * a.q_heads + r % a.group;
+        }
+        const float* lse = a.lse + (int64_t)(w.begin + q0 * a.tile_tokens) * a.q_heads + h * a.group;
+        auto fetch = [&](int i) {
+            const float* l = lse + (int64_t)i * a.tile_tokens * a.q_heads;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) next[k] = token[k] < w.count - i * a.tile_tokens ? l[at[k]] : -INFINITY;
+        };
+        fetch(0);
         bool ok = true;
         for (int i = 0; i < num; ++i) {
             float v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int r = lane + 32 * k, token = (q0 + i) * a.tile_tokens + r / a.group;
-                v[k] = -INFINITY;
-                if (r < rows && token < w.count) {
-                    const float lse = a.lse[(int64_t)(w.begin + token) * a.q_heads + h * a.group + r % a.group];
-                    if (lse != -INFINITY) v[k] = (float)((double)lse * -1.44269504088896340736);
-                }
-            }
-            // slot i % 4 may be written once tile i - 4 has been read; waiting for tile i - 2, whose buffer hand-back is the latest that can have happened, is enough
-            if (i >= 2)
-                for (int t = 0; t < tiles && ok; ++t) ok = mbar_wait(&bars->s_empty[t][i & 1], ((i >> 1) & 1) ^ 1, abort_flag, status, 25);
-            ok = __all_sync(~0u, ok);
+            for (int k = 0; k < 4; ++k) v[k] = next[k] == -INFINITY ? -INFINITY : -fmaf(next[k], kHi, next[k] * kLo);
+            fetch(i + 1);                                                       // (behind the last: no row is valid, nothing is read)
+            // Slot i % 4 may be written once tile i - 4 has been read.  Score buffers are handed back before the values of their slot are read, so tile i - 4 is surely done
+            // when the buffer of tile i - 2 comes back, the latest that can have happened by now.
+            if (i >= 2) ok = __all_sync(~0u, mbar_wait_near(&bars->s_empty[i & 1], ((i >> 1) & 1) ^ 1, abort_flag, status, 25));
             if (!ok) break;
 #pragma unroll
             for (int k = 0; k < 4; ++k) l_ring[(i & 3) * 128 + lane + 32 * k] = v[k];
@@ -603,72 +599,66 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
         }
     } else if (warp < kWeighWarps) {
         // -------------------------------------------------------------------- a thread owns a token and half of the rows
-        const int t = (warp >> 2) & 1, half = warp >> 3;
+        const int half = warp >> 2;
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint64_t cc = pair2(a.scale_log2, a.scale_log2);
         bool ok = true;
-        if (t < tiles) {
-            for (int i = 0; i < num; ++i) {
-                const int buf = i & 1, tok0 = (q0 + i) * a.tile_tokens;
-                ok = __all_sync(~0u, mbar_wait(&bars->l_full[i & 3], (i >> 2) & 1, abort_flag, status, 26) &&
-                                     mbar_wait_near(&bars->s_full[t][buf], (i >> 1) & 1, abort_flag, status, 27));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t addr = tmem + lane_addr + 256u * t + 128u * buf + 64u * half;
-                const float* lr = l_ring + (i & 3) * 128 + 64 * half;
-                // columns of rows that see this token: [cl, ch)
-                const int valid = min(rows, (w.count - tok0) * a.group);
-                int cl = 0, ch = valid;
-                if (a.causal) cl = max(0, key - off - tok0) * a.group;
-                if (a.window) ch = (int)min((int64_t)valid, max((int64_t)0, (int64_t)key - off + a.window - tok0) * a.group);
-                const bool whole = __all_sync(~0u, cl == 0 && ch >= 128);
-                const uint64_t cc = pair2(a.scale_log2, a.scale_log2);
-                uint32_t s[2][32];
-                tmem_ld32(addr, s[0]);
-                tmem_ld32(addr + 32, s[1]);
+        for (int i = 0; i < num; ++i) {
+            const int buf = i & 1, tok0 = (q0 + i) * a.tile_tokens;
+            ok = __all_sync(~0u, mbar_wait_near(&bars->l_full[i & 3], (i >> 2) & 1, abort_flag, status, 26) &&
+                                 mbar_wait_near(&bars->s_full[buf], (i >> 1) & 1, abort_flag, status, 27));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t addr = tmem + lane_addr + 128u * buf + 64u * half;
+            const float* lr = l_ring + (i & 3) * 128 + 64 * half;
+            // columns of rows that see this token: [cl, ch)
+            const int valid = min(rows, (w.count - tok0) * a.group);
+            int cl = 0, ch = valid;
+            if (a.causal) cl = max(0, key - off - tok0) * a.group;
+            if (a.window) ch = (int)min((int64_t)valid, max((int64_t)0, (int64_t)key - off + a.window - tok0) * a.group);
+            const bool whole = __all_sync(~0u, cl == 0 && ch >= 128);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t s[32];
+                tmem_ld32(addr + 32 * k, s);
                 tmem_wait_ld();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars->s_empty[t][buf]);
+                if (k == 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars->s_empty[buf]);
+                }
                 if (whole) {
                     uint64_t sum[2] = {0, 0};
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int x = 0; x < 32; x += 4) {
-                            const float4 lv = *(const float4*)(lr + 32 * k + x);
-                            const uint64_t e0 = fma2(pair2(__uint_as_float(s[k][x]), __uint_as_float(s[k][x + 1])), cc, pair2(lv.x, lv.y));
-                            const uint64_t e1 = fma2(pair2(__uint_as_float(s[k][x + 2]), __uint_as_float(s[k][x + 3])), cc, pair2(lv.z, lv.w));
-                            sum[0] = add2(sum[0], ex2_mufu(e0));
-                            sum[1] = add2(sum[1], kWeighPoly && x % (4 * (kWeighPoly ? kWeighPoly : 1)) == 0 ? ex2_pair(e1) : ex2_mufu(e1));
-                        }
+                    for (int x = 0; x < 32; x += 4) {
+                        const float4 lv = *(const float4*)(lr + 32 * k + x);
+                        sum[0] = add2(sum[0], ex2_mufu(fma2(pair2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), cc, pair2(lv.x, lv.y))));
+                        sum[1] = add2(sum[1], ex2_mufu(fma2(pair2(__uint_as_float(s[x + 2]), __uint_as_float(s[x + 3])), cc, pair2(lv.z, lv.w))));
+                    }
                     const float2 p = split2(add2(sum[0], sum[1]));
                     acc += p.x + p.y;
-                } else if (64 * half < valid) {
+                } else if (64 * half + 32 * k < valid) {
+                    const uint32_t see = col_mask(cl, ch, 64 * half + 32 * k);
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const uint32_t see = col_mask(cl, ch, 64 * half + 32 * k);
-                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) {
-                            const float p = ex2f(fmaf(__uint_as_float(s[k][x]), a.scale_log2, lr[32 * k + x]));
-                            sum[x & 3] += (see >> x) & 1 ? p : 0.f;
-                        }
-                        acc += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    for (int x = 0; x < 32; ++x) {
+                        const float p = ex2f(fmaf(__uint_as_float(s[x]), a.scale_log2, lr[32 * k + x]));
+                        sum[x & 3] += (see >> x) & 1 ? p : 0.f;
                     }
+                    acc += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 }
             }
-            if (!ok) acc = 0.f;
         }
-        if (half) s_acc[t * 128 + (warp & 3) * 32 + lane] = acc;
+        if (half) s_acc[(warp & 3) * 32 + lane] = acc;
     }
     tc_fence_before();
     __syncthreads();
-    if (warp < 8 && key < w.n && !*abort_flag) {
+    if (warp < 4 && key < w.n && !*abort_flag) {
         const int64_t at = ((int64_t)b * a.heads + h) * a.w_stride + key;
         a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + (acc + s_acc[key - key0]);
     }
     if (warp == kWeighWarps) {
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kWeighCols) : "memory");
     }
 }
 
@@ -684,9 +674,9 @@ cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorM
 }
 template <class T, int D>
 cudaError_t weigh_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(k_weigh<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeighSmem<D>::kBytes);
+    cudaError_t e = cudaFuncSetAttribute(k_weigh<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, GeoWeigh<D>::kSmem);
     if (e != cudaSuccess) return e;
-    k_weigh<T, D><<<dim3((unsigned)ceil_div(a.batch.max_len, 256), a.heads, a.batch.batch), kThreadsWe, WeighSmem<D>::kBytes, stream>>>(mq, mk, a);
+    k_weigh<T, D><<<dim3((unsigned)ceil_div(a.batch.max_len, 128), a.heads, a.batch.batch), kThreadsWe, GeoWeigh<D>::kSmem, stream>>>(mq, mk, a);
     ++g_launches;
     return cudaGetLastError();
 }

@@ -92,3 +92,20 @@ def test_rotary_refuses(fd, kw, status):
                           a["scale"], 0, None, err, 256)
     assert st == status and err.value
     assert fd.fd_launch_count() == 0
+
+
+def test_packed_arguments(fd):
+    """The formats that the binding packs in one step are the structures of the header, field by field."""
+    from paper_2609_38198_b200 import binding as b
+    values = iter(range(1, 100))
+    for fmt, st in ((b._HEADS, b.fd_heads), (b._APPEND, b.fd_kv_append_args), (b._ATTEND, b.fd_kv_attend_args), (b._EVICT, b.fd_kv_evict_args)):
+        assert fmt.size == ctypes.sizeof(st)
+
+        def fields(t):
+            return [x for n, f in t._fields_ for x in (fields(f) if issubclass(f, ctypes.Structure) else [n])]
+
+        def read(o):
+            return [x for n, f in o._fields_ for x in (read(getattr(o, n)) if issubclass(f, ctypes.Structure) else [getattr(o, n)])]
+
+        want = [next(values) for _ in fields(st)]
+        assert read(st.from_buffer_copy(fmt.pack(*want))) == want
