@@ -46,7 +46,9 @@ bool make_map(CUtensorMap* m, void* base, int dtype, int rank, const uint64_t* d
     for (int i = 0; i < rank; ++i) { d[i] = dims[i]; b[i] = box[i]; }
     for (int i = 0; i + 1 < rank; ++i) s[i] = (cuuint64_t)strides[i] * 2;
     return fn(m, dtype == FD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, base, d, s, b, one,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              d[0] > 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,      // (a row of a head, not of its neighbour)
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 constexpr int64_t kMaxStride = (int64_t)1 << 38;      // (a tensor map's strides end at 2^40 bytes)
@@ -108,29 +110,30 @@ bool same(const fd_heads& a, const fd_heads& b) { return a.p_dev == b.p_dev && a
 
 }  // namespace
 
-// Few rows a sequence: one row tile of 16, bound by the cache's bytes.  The cache is cut into parts of 256 tokens or more until four rounds of CTAs (two fit an
-// SM) run, so that uneven lengths even out.  Else: parts of at least two tiles of 128, as many as fill the GPU once if every sequence were as long as the longest.
+// Few rows a sequence: as many CTAs as the GPU holds at once (two an SM), each with 64 tokens of a cache or more, share the caches evenly.  Else: the cache in parts of
+// at least two tiles of 128, as many as fill the GPU once if every sequence were as long as the longest.
 Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weights) {
     Plan p{};
     const int64_t heads = kv->d.heads, group = q_heads / heads, sms = kv->sm_count, live = std::min(b->batch, b->total_q);
+    const size_t rows = (size_t)b->total_q * q_heads, dim = kv->d.head_dim;
+    p.splits = 1;
     p.few = (int64_t)b->max_new * group <= kFewRows;
-    const int64_t unit = p.few ? 64 : 128, tiles = std::max<int64_t>(1, ceil_div(b->max_len, unit));
-    int64_t s;
     if (p.few) {
-        s = std::max<int64_t>(1, std::min(ceil_div(8 * sms, live * heads), tiles / 4));
-    } else {
-        const int64_t ctas = (b->total_q / (2 * (128 / group)) + live) * heads;
-        s = std::max<int64_t>(1, std::min(sms / ctas, tiles / 2));
+        p.ctas = (int)std::min<int64_t>(2 * sms, live * heads * std::max<int64_t>(1, ceil_div(b->max_len, 64)));
+        p.parts = (size_t)round_up(2 * (int64_t)b->batch * heads, 4);
+        p.part_o = (size_t)2 * p.ctas * kFewRows * dim;
+        p.part_lse = (size_t)2 * p.ctas * kFewRows;
+        if (weights) {
+            p.score_stride = round_up(b->max_len, 64);
+            p.scores = (size_t)b->batch * heads * kFewRows * p.score_stride;
+        }
+        return p;
     }
-    s = std::min<int64_t>(s, kMaxSplits);
+    const int64_t tiles = std::max<int64_t>(1, ceil_div(b->max_len, 128)), ctas = (b->total_q / (2 * (128 / group)) + live) * heads;
+    const int64_t s = std::max<int64_t>(1, std::min<int64_t>(std::min(sms / ctas, tiles / 2), kMaxSplits));
     p.split_tiles = (int)ceil_div(tiles, s);
     p.splits = (int)ceil_div(tiles, p.split_tiles);
-    const size_t rows = (size_t)b->total_q * q_heads;
-    if (p.splits > 1) { p.part_o = (size_t)p.splits * rows * kv->d.head_dim; p.part_lse = (size_t)p.splits * rows; }
-    if (p.few && weights) {
-        p.score_stride = round_up(b->max_len, 64);
-        p.scores = (size_t)b->batch * heads * kFewRows * p.score_stride;
-    }
+    if (p.splits > 1) { p.part_o = p.splits * rows * dim; p.part_lse = (p.splits * rows + 3) / 4 * 4; }
     return p;
 }
 
@@ -277,8 +280,7 @@ fd_status fd_kv_append(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_append
 
 size_t fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* b, int32_t q_heads, int32_t weights) {
     if (!kv || !b || q_heads < 1 || q_heads % kv->d.heads || q_heads / kv->d.heads > 128 || b->batch < 1 || b->total_q < 1) return 0;
-    const Plan p = plan_attend(kv, b, q_heads, weights != 0);
-    return (p.part_o + p.part_lse + p.scores) * sizeof(float);
+    return plan_attend(kv, b, q_heads, weights != 0).bytes();
 }
 
 fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend_args* x, void* workspace_dev, size_t workspace_bytes, void* cuda_stream,
@@ -320,14 +322,15 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
     bool few = false;
     if (b->total_q > 0) {
         const Plan p = plan_attend(kv, b, a.q_heads, a.w_out != nullptr);
-        const size_t need = (p.part_o + p.part_lse + p.scores) * sizeof(float);
+        const size_t need = p.bytes();
         if (need && (!workspace_dev || workspace_bytes < need)) return err(FD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
         if (need && (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return err(FD_ERR_INVALID, "workspace must be 16-byte aligned");
         few = p.few;
-        a.splits = p.splits; a.split_tiles = p.split_tiles;
-        a.part_o = static_cast<float*>(workspace_dev);
-        a.scores = p.scores ? a.part_o + p.part_o : nullptr; a.score_stride = p.score_stride;
-        a.part_lse = a.part_o + p.part_o + p.scores;
+        a.splits = p.splits; a.split_tiles = p.split_tiles; a.ctas = p.ctas; a.few_rows = b->max_new * a.group;
+        a.parts = static_cast<int2*>(workspace_dev);
+        a.part_o = static_cast<float*>(workspace_dev) + p.parts;
+        a.part_lse = a.part_o + p.part_o;
+        a.scores = p.scores ? a.part_lse + p.part_lse : nullptr; a.score_stride = p.score_stride;
         a.q = heads_of(x->q);
         cudaError_t e;
         if (few) {

@@ -1,5 +1,5 @@
 // Internal declarations of the paged cache's operators (fd_kv.cu: entry points; fd_kv_rows.cu: rotary positions, append, eviction;
-// fd_kv_attend.cu: attention and its column sums; fd_kv_decode.cu: attention of few rows; fd_kv_join.cu: what follows both).
+// fd_kv_attend.cu: attention and its column sums; fd_kv_decode.cu: attention of few rows).
 #pragma once
 
 #include <cuda.h>
@@ -16,8 +16,24 @@ struct fd_kv {
     CUtensorMap few_k, few_v;
 };
 
+#include <atomic>
+
 namespace fd {
 namespace kv {
+
+// Lets a kernel have `bytes` of dynamic shared memory on the current device; asks the runtime once per kernel and device (0.5 us a call).
+template <auto KERNEL>
+cudaError_t allow_smem(size_t bytes) {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // Bits of a cache's first status word; the second holds the code of a wait that ran out.
 constexpr unsigned kBadPage = 1, kBadLength = 2;
@@ -79,8 +95,10 @@ struct AttendArgs {
     float scale_log2;                // scale * log2(e)
     float* lse;
     const float* w_in; float* w_out; int64_t w_stride;
-    int splits, split_tiles;         // the cache in `splits` parts of split_tiles tiles (of 128 tokens; of 64 with few rows)
-    float* part_o; float* part_lse;  // [split][token][query head]([head_dim])
+    int splits, split_tiles;         // many rows: the cache in `splits` parts of split_tiles tiles of 128 tokens
+    int ctas, few_rows;              // few rows: CTAs that share the batch's caches; rows a sequence has at most; first CTA and number of the parts of each
+    int2* parts;                     // (sequence, head)
+    float* part_o; float* part_lse;  // [split][token][query head]([head_dim]); few rows: [slot][kFewRows]([head_dim])
     float* scores; int64_t score_stride;     // few rows and weights: scale_log2 q.k of every row and slot, [sequence][head][kFewRows][score_stride]
     int box_rows;
     const void* v_pool; int64_t v_page, v_token, v_head;
@@ -92,15 +110,15 @@ constexpr int kMaxSplits = 1024;         // parts of a cache
 // How the work of a call is cut, and what its workspace holds.
 struct Plan {
     bool few;
-    int splits, split_tiles;
+    int splits, split_tiles, ctas;
     int64_t score_stride;
-    size_t part_o, part_lse, scores;         // floats
+    size_t parts, part_o, part_lse, scores;         // in floats, in this order, each a multiple of 4
+    size_t bytes() const { return (parts + part_o + part_lse + scores) * sizeof(float); }
 };
 Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weights);
 cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream);
 cudaError_t launch_weigh(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream);
 cudaError_t launch_few(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream);
-cudaError_t launch_join(const AttendArgs& a, cudaStream_t stream);
 
 }  // namespace kv
 }  // namespace fd

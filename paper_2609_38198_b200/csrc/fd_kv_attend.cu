@@ -54,7 +54,6 @@ __device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, v
         }
     return true;
 }
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // Instruction descriptor, fp32 accumulation, M = 128; `mn`: the B operand is MN-major.
 template <class T> constexpr uint32_t idesc_kv(int n, bool mn) {
     return (1u << 4) | (Elem<T>::kFormat << 7) | (Elem<T>::kFormat << 10) | ((mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
@@ -146,6 +145,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     volatile int* abort_flag = &bars->abort_flag;
     unsigned int* status = a.batch.status + 1;
 
+    grid_wait();
+    grid_go();
     // work items: split fastest, then head, then token group, the last groups (which see most) first
     const int split = blockIdx.x % a.splits, h = (blockIdx.x / a.splits) % a.heads;
     const int groups = gridDim.x / (a.splits * a.heads), slot = groups - 1 - blockIdx.x / (a.splits * a.heads);
@@ -453,6 +454,76 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     }
 }
 
+// Joins the parts of the cache: out = sum_s 2^(lse_s - lse) o_s.  Few parts: a warp a row; many: the eight warps of a block share the parts of one
+// row (147 parts of 56 rows: a warp a row took 70 us, one wait for memory after the other).  The parts' factors are made in parallel first.
+template <class T, int D, int W>
+__global__ void __launch_bounds__(256) k_join(const AttendArgs a) {
+    constexpr int E = D / 32;
+    __shared__ float s_f[W == 1 ? 8 * 32 : kMaxSplits];
+    __shared__ float s_o[W == 1 ? 1 : 8 * D], s_top[8], s_sum[8];
+    grid_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, me = W == 1 ? lane : (int)threadIdx.x;
+    const int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + warp : blockIdx.x;
+    const int64_t rows = (int64_t)q_begin(a.batch, a.batch.batch) * a.q_heads, all = (int64_t)a.batch.total_q * a.q_heads;
+    if (row >= rows) return;
+    float* f = W == 1 ? s_f + 32 * warp : s_f;
+    float top = -INFINITY;
+    for (int s = me; s < a.splits; s += 32 * W) top = max_nan(top, f[s] = a.part_lse[s * all + row]);
+    for (int o = 16; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(~0u, top, o));
+    if (W > 1) {
+        if (lane == 0) s_top[warp] = top;
+        __syncthreads();
+        for (int k = 0; k < 8; ++k) top = max_nan(top, s_top[k]);
+    }
+    float sum = 0.f;
+    if (top != -INFINITY)
+        for (int s = me; s < a.splits; s += 32 * W) sum += f[s] = ex2f(f[s] - top);           // (a part without rows in sight: 0)
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (W > 1) {
+        if (lane == 0) s_sum[warp] = sum;
+        __syncthreads();
+        sum = 0.f;
+        for (int k = 0; k < 8; ++k) sum += s_sum[k];
+    } else __syncwarp();
+    float o[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] = 0.f;
+    if (top != -INFINITY) {
+        const float* p = a.part_o + row * D + lane * E;
+#pragma unroll 4
+        for (int s = W == 1 ? 0 : warp; s < a.splits; s += W) {
+            const float w = f[s];
+            if (w == 0.f) continue;                                // (its o may not have been written)
+            const float* q = p + s * all * D;
+            if (E == 4) {
+                const float4 v = *(const float4*)q;
+                o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]); o[E - 2] = fmaf(w, v.z, o[E - 2]); o[E - 1] = fmaf(w, v.w, o[E - 1]);
+            } else {
+                const float2 v = *(const float2*)q;
+                o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]);
+            }
+        }
+    }
+    if (W > 1) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) s_o[warp * D + lane * E + i] = o[i];
+        __syncthreads();
+        if (warp) return;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            o[i] = 0.f;
+            for (int k = 0; k < 8; ++k) o[i] += s_o[k * D + lane * E + i];
+        }
+    }
+    const float inv = top == -INFINITY ? 0.f : 1.0f / sum;
+    const int64_t token = row / a.q_heads;
+    const int head = (int)(row - token * a.q_heads);
+    uint32_t* dst = (uint32_t*)((T*)a.out.p + token * a.out.token_stride + head * a.out.head_stride + lane * E);
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) dst[i] = Elem<T>::pack(o[2 * i] * inv, o[2 * i + 1] * inv);
+    if (a.lse && lane == 0) a.lse[row] = top == -INFINITY ? -INFINITY : (float)((double)(top + log2f(sum)) * 0.69314718055994530942);
+}
+
 // k_weigh: what every cached token received, w_j += sum over rows of 2^(c s - lse).  One CTA takes a tile of 128 cached tokens as the M side (S^T = K Q^T: a thread
 // owns a token, so the sum over rows is a sum over its columns and needs no exchange) and goes through the rows that see them, 128 at a
 // time; two warpgroups share the columns.  The exponentials bound it.  Two CTAs an SM fill each other's waits and even out the lengths: with
@@ -485,6 +556,8 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     volatile int* abort_flag = &bars->abort_flag;
     unsigned int* status = a.batch.status + 1;
 
+    grid_wait();
+    grid_go();
     const int h = blockIdx.y, b = blockIdx.z, key0 = blockIdx.x * 128;
     Work w;
     w.b = b; w.begin = q_begin(a.batch, b); w.count = max(0, q_begin(a.batch, b + 1) - w.begin); w.n = kv_length(a.batch, b, false); w.t0 = 0;
@@ -664,21 +737,23 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
 
 template <class T, int D>
 cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(k_attend<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<D>::kSmem);
+    cudaError_t e = allow_smem<k_attend<T, D>>(Geo<D>::kSmem);
     if (e != cudaSuccess) return e;
     const int64_t groups = a.batch.total_q / (2 * a.tile_tokens) + std::min(a.batch.batch, a.batch.total_q);
-    k_attend<T, D><<<(unsigned)(groups * a.heads * a.splits), kThreadsAt, Geo<D>::kSmem, stream>>>(mq, mk, mv, a);
     ++g_launches;
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return a.splits > 1 ? launch_join(a, stream) : cudaSuccess;
+    if ((e = launch_behind(stream, dim3((unsigned)(groups * a.heads * a.splits)), dim3(kThreadsAt), Geo<D>::kSmem, k_attend<T, D>, mq, mk, mv, a)) != cudaSuccess) return e;
+    if (a.splits == 1) return cudaSuccess;
+    const int64_t rows = (int64_t)a.batch.total_q * a.q_heads;
+    ++g_launches;
+    if (a.splits > 16) return launch_behind(stream, dim3((unsigned)rows), dim3(256), 0, k_join<T, D, 8>, a);
+    return launch_behind(stream, dim3((unsigned)ceil_div(rows, 8)), dim3(256), 0, k_join<T, D, 1>, a);
 }
 template <class T, int D>
 cudaError_t weigh_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(k_weigh<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, GeoWeigh<D>::kSmem);
+    cudaError_t e = allow_smem<k_weigh<T, D>>(GeoWeigh<D>::kSmem);
     if (e != cudaSuccess) return e;
-    k_weigh<T, D><<<dim3((unsigned)ceil_div(a.batch.max_len, 128), a.heads, a.batch.batch), kThreadsWe, GeoWeigh<D>::kSmem, stream>>>(mq, mk, a);
     ++g_launches;
-    return cudaGetLastError();
+    return launch_behind(stream, dim3((unsigned)ceil_div(a.batch.max_len, 128), a.heads, a.batch.batch), dim3(kThreadsWe), GeoWeigh<D>::kSmem, k_weigh<T, D>, mq, mk, a);
 }
 
 }  // namespace

@@ -29,6 +29,8 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
     extern __shared__ float2 turn[];                         // [block_tokens][rot / 2]
     __shared__ int64_t place[16][2];                         // pool offset of a token's key and value row of head 0, -1: nowhere
     using V = Vec<T, VEC>;
+    grid_wait();
+    grid_go();
     const int t0 = blockIdx.x * block_tokens, nt = min(block_tokens, a.tokens - t0);
     const int half = a.rot / 2;
     for (int i = threadIdx.x; i < nt * half; i += kRowThreads) {
@@ -143,10 +145,8 @@ cudaError_t launch_rows_t(const RowsArgs& a, int sm_count, cudaStream_t stream) 
     while (block_tokens == 1 && shares < 8 && (int64_t)a.tokens * shares < 2 * sm_count && per_token > kRowThreads * shares) shares *= 2;
     const dim3 grid((unsigned)ceil_div(a.tokens, block_tokens), (unsigned)shares);
     const size_t smem = (size_t)block_tokens * (a.rot / 2) * sizeof(float2);
-    if (a.layout == FD_ROTARY_HALF) k_rows<T, VEC, true><<<grid, kRowThreads, smem, stream>>>(a, block_tokens);
-    else k_rows<T, VEC, false><<<grid, kRowThreads, smem, stream>>>(a, block_tokens);
     ++g_launches;
-    return cudaGetLastError();
+    return launch_behind(stream, grid, dim3(kRowThreads), smem, a.layout == FD_ROTARY_HALF ? k_rows<T, VEC, true> : k_rows<T, VEC, false>, a, block_tokens);
 }
 template <class T>
 cudaError_t launch_rows_any(const RowsArgs& a, int sm_count, cudaStream_t stream) {
@@ -176,6 +176,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
     __shared__ unsigned hist[2048];
     __shared__ unsigned warp_total[kSelWarps], s_bin, s_left;
     __shared__ unsigned warp_above[kSelWarps], warp_equal[kSelWarps];
+    grid_wait();
     grid_go();
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int n = kv_length(a.batch, b, true);
@@ -312,6 +313,7 @@ template <int D>
 __global__ void __launch_bounds__(kMoveThreads) k_move(const EvictArgs a, const int shares, const bool write_len) {
     const int h = blockIdx.y, b = blockIdx.z;
     grid_wait();
+    grid_go();
     const Batch& B = a.batch;
     const int n = kv_length(B, b, false), count = min(n, a.keep);
     const int* kept = a.kept + ((int64_t)b * a.heads + h) * a.keep;
@@ -374,11 +376,10 @@ cudaError_t launch_rows(const RowsArgs& a, int dtype, int sm_count, cudaStream_t
 
 cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream) {
     const size_t smem = sizeof(unsigned) * (size_t)(a.batch.max_len < kSelKeys ? a.batch.max_len : kSelKeys);
-    cudaError_t e = cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeys * sizeof(unsigned));
+    cudaError_t e = allow_smem<k_select>(kSelKeys * sizeof(unsigned));
     if (e != cudaSuccess) return e;
-    k_select<<<dim3(a.heads, a.batch.batch), kSelThreads, smem, stream>>>(a);
     ++g_launches;
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_behind(stream, dim3(a.heads, a.batch.batch), dim3(kSelThreads), smem, k_select, a)) != cudaSuccess) return e;
     const bool over = a.new_len < a.batch.kv_len + a.batch.batch && a.batch.kv_len < a.new_len + a.batch.batch;
     // blocks for about 16 KB in flight on every SM twice over, of 64 rows or more; in place as many as a row has slices of 64 bytes do work
     int shares = a.head_dim / 32;
