@@ -163,7 +163,7 @@ cudaError_t launch_rows_any(const RowsArgs& a, int sm_count, cudaStream_t stream
 // it from the top.  (Two bits at a time, by counting the keys at or above three candidates, needs 16 rounds of a barrier each: 600 keys took 12.5 us, now 9.)  Then each
 // warp counts, and after a scan over the warps writes down, the kept slots of its stretch in order: all keys above the found one, the first of those
 // equal to it.
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kSelKeys = 40960;
+constexpr int kSelKeys = 40960;
 
 __device__ __forceinline__ unsigned weight_key(float w) {
     if (w != w) return 0u;                                   // NaN: below every number
@@ -171,7 +171,10 @@ __device__ __forceinline__ unsigned weight_key(float w) {
     return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 
+// 512 threads up to 4096 tokens (1100 tokens: 9.8 us a call against 10.9 with 1024), 1024 beyond (8192 tokens: 45.9 us against 50.2).
+template <int kSelThreads>
 __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
+    constexpr int kSelWarps = kSelThreads / 32, kSelBins = 2048 / kSelThreads;
     extern __shared__ unsigned s_key[];
     __shared__ unsigned hist[2048];
     __shared__ unsigned warp_total[kSelWarps], s_bin, s_left;
@@ -206,10 +209,10 @@ __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
             if (pass == 0 || (k >> (pass == 1 ? 21 : 10)) == (found >> (pass == 1 ? 21 : 10))) atomicAdd(&hist[(k >> shift) & mask], 1u);
         }
         __syncthreads();
-        // bins from the top, 4 a thread: the one in which the want-th largest lies
-        unsigned c[4], sum = 0;
+        // bins from the top, a few a thread: the one in which the want-th largest lies
+        unsigned c[kSelBins], sum = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum += c[j] = hist[2047 - 4 * tid - j];
+        for (int j = 0; j < kSelBins; ++j) sum += c[j] = hist[2047 - kSelBins * tid - j];
         unsigned upto = sum;
         for (int o = 1; o < 32; o <<= 1) { const unsigned v = __shfl_up_sync(~0u, upto, o); if (lane >= o) upto += v; }
         if (lane == 31) warp_total[warp] = upto;
@@ -217,8 +220,8 @@ __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
         for (int j = 0; j < warp; ++j) upto += warp_total[j];
         unsigned before = upto - sum;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (before < want && want <= before + c[j]) { s_bin = 2047 - 4 * tid - j; s_left = want - before; }
+        for (int j = 0; j < kSelBins; ++j) {
+            if (before < want && want <= before + c[j]) { s_bin = 2047 - kSelBins * tid - j; s_left = want - before; }
             before += c[j];
         }
         __syncthreads();
@@ -227,6 +230,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
     }
     const int stretch = (len + kSelThreads - 1) / kSelThreads * 32, i0 = warp * stretch, i1 = min(len, i0 + stretch);
     unsigned above = 0, equal = 0;
+#pragma unroll 4
     for (int i = i0; i < i1; i += 32) {
         const unsigned k = i + lane < i1 ? key(i + lane) : 0u;
         above += __popc(__ballot_sync(~0u, i + lane < i1 && k > found));
@@ -240,6 +244,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
         if (j < warp) { above_before += warp_above[j]; equal_before += warp_equal[j]; }
     }
     const unsigned take = left - all_above;                              // of the equal ones
+#pragma unroll 4
     for (int i = i0; i < i1; i += 32) {
         const bool in = i + lane < i1;
         const unsigned k = in ? key(i + lane) : 0u, below = (1u << lane) - 1;
@@ -257,7 +262,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
 // time.  In place: every block takes a slice of 64 bytes of all rows, since slices move independently; a wave of rows is read, the block waits,
 // and the wave is written.  Row r comes from slot kept[r] >= r, so later waves read nothing that was written.  Three waves are under way at
 // once in both: the slots of the next but one, the pages of the next, the rows of this.  One more block a head moves the weights, in waves as well.
-constexpr int kMoveThreads = 256, kMoveDepth = 4;
+constexpr int kMoveThreads = 256, kMoveDepth = 2;
 
 template <int LANES, bool IN_PLACE>
 __device__ __forceinline__ void move_rows(const EvictArgs& a, uint16_t* pool, int64_t page_s, int64_t token_s, const int* kept, const int* from, const int* to, int r0, int room) {
@@ -315,22 +320,23 @@ __global__ void __launch_bounds__(kMoveThreads) k_move(const EvictArgs a, const 
     grid_wait();
     grid_go();
     const Batch& B = a.batch;
-    const int n = kv_length(B, b, false), count = min(n, a.keep);
     const int* kept = a.kept + ((int64_t)b * a.heads + h) * a.keep;
     if ((int)blockIdx.x == 2 * shares) {
+        const int n = kv_length(B, b, false), count = min(n, a.keep);
         if (write_len && h == 0 && threadIdx.x == 0) a.new_len[b] = count;
         const float* w = a.w_in + ((int64_t)b * a.heads + h) * a.w_stride;
         float* out = a.w_out + ((int64_t)b * a.heads + h) * a.w_stride;
-        for (int r0 = 0; r0 < n; r0 += kMoveDepth * kMoveThreads) {
-            float v[kMoveDepth];
+        constexpr int kDeep = 4;
+        for (int r0 = 0; r0 < n; r0 += kDeep * kMoveThreads) {
+            float v[kDeep];
 #pragma unroll
-            for (int u = 0; u < kMoveDepth; ++u) {
+            for (int u = 0; u < kDeep; ++u) {
                 const int r = r0 + u * kMoveThreads + threadIdx.x;
                 v[u] = r < count ? w[kept[r]] : 0.f;
             }
             __syncthreads();
 #pragma unroll
-            for (int u = 0; u < kMoveDepth; ++u) {
+            for (int u = 0; u < kDeep; ++u) {
                 const int r = r0 + u * kMoveThreads + threadIdx.x;
                 if (r < n) out[r] = v[u];
             }
@@ -343,17 +349,12 @@ __global__ void __launch_bounds__(kMoveThreads) k_move(const EvictArgs a, const 
     uint16_t* pool = (uint16_t*)(val ? a.v_pool : a.k_pool) + h * (val ? a.v_head : a.k_head);
     const int* from = B.table + b * B.table_stride;
     const int* to = a.new_table + b * a.new_table_stride;
-    const int room = (int)min((int64_t)a.new_max_pages * B.page_size, (int64_t)count);
-    if (room < count && threadIdx.x == 0) atomicOr(B.status, kBadLength);
-    // in place: the two tables agree somewhere (where one does not end before the other)
-    const int both = min((room + B.page_size - 1) / B.page_size, B.max_pages);
-    bool agree = false;
-    for (int i = threadIdx.x; i < both; i += kMoveThreads) agree |= from[i] == to[i];
-    if (__syncthreads_or(agree)) {
-        if (share < D / 32) move_rows<4, true>(a, pool + share * 32, page_s, token_s, kept, from, to, 0, room);
+    // (kept holds -1 behind the last row, so no length is waited for; the tables are the same or have no page in common, so their first pages tell)
+    if (from[0] == to[0]) {
+        if (share < D / 32) move_rows<4, true>(a, pool + share * 32, page_s, token_s, kept, from, to, 0, a.keep);
     } else {
-        const int per = (room + shares - 1) / shares;
-        move_rows<D / 8, false>(a, pool, page_s, token_s, kept, from, to, share * per, min(room, (share + 1) * per));
+        const int per = (a.keep + shares - 1) / shares;
+        move_rows<D / 8, false>(a, pool, page_s, token_s, kept, from, to, share * per, min(a.keep, (share + 1) * per));
     }
 }
 
@@ -376,10 +377,12 @@ cudaError_t launch_rows(const RowsArgs& a, int dtype, int sm_count, cudaStream_t
 
 cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream) {
     const size_t smem = sizeof(unsigned) * (size_t)(a.batch.max_len < kSelKeys ? a.batch.max_len : kSelKeys);
-    cudaError_t e = allow_smem<k_select>(kSelKeys * sizeof(unsigned));
+    const bool many = a.batch.max_len > 4096;
+    cudaError_t e = many ? allow_smem<k_select<1024>>(kSelKeys * sizeof(unsigned)) : allow_smem<k_select<512>>(kSelKeys * sizeof(unsigned));
     if (e != cudaSuccess) return e;
     ++g_launches;
-    if ((e = launch_behind(stream, dim3(a.heads, a.batch.batch), dim3(kSelThreads), smem, k_select, a)) != cudaSuccess) return e;
+    e = launch_behind(stream, dim3(a.heads, a.batch.batch), dim3(many ? 1024 : 512), smem, many ? k_select<1024> : k_select<512>, a);
+    if (e != cudaSuccess) return e;
     const bool over = a.new_len < a.batch.kv_len + a.batch.batch && a.batch.kv_len < a.new_len + a.batch.batch;
     // blocks for about 16 KB in flight on every SM twice over, of 64 rows or more; in place as many as a row has slices of 64 bytes do work
     int shares = a.head_dim / 32;
