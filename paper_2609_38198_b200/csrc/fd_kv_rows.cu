@@ -24,8 +24,16 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __
 
 template <class T, int VEC> struct alignas(VEC * sizeof(T)) Vec { T v[VEC]; };
 
-template <class T, int VEC, bool HALF>
-__global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const int block_tokens) {
+// A row that is read once (8192 tokens of 32 heads: 28.3 -> 27.2 us; the results are left to the cache, for what reads them next.  Appends lose 2 us of 44 by it).
+template <class V> __device__ __forceinline__ V load_once(const void* p) {
+    if constexpr (sizeof(V) == 16) {
+        const uint4 x = __ldcs((const uint4*)p);
+        return *(const V*)&x;
+    } else return *(const V*)p;
+}
+
+template <class T, int VEC, bool HALF, bool APPEND>
+__global__ void __launch_bounds__(kRowThreads, APPEND ? 8 : 6) k_rows(const RowsArgs a, const int block_tokens) {
     extern __shared__ float2 turn[];                         // [block_tokens][rot / 2]
     __shared__ int64_t place[16][2];                         // pool offset of a token's key and value row of head 0, -1: nowhere
     using V = Vec<T, VEC>;
@@ -40,7 +48,7 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
         turn[i] = make_float2(c * a.scale, s * a.scale * a.sign);
     }
-    if (a.append && threadIdx.x < nt) {
+    if (APPEND && threadIdx.x < nt) {
         const Batch& B = a.batch;
         const int t = t0 + threadIdx.x;
         int lo = 0, hi = B.batch;                            // last sequence that begins at or before t
@@ -63,7 +71,7 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
     }
     __syncthreads();
     const int unit_count = a.head_dim / (2 * VEC), turned = a.rot / (2 * VEC);
-    const int heads = a.x.heads + (a.append ? a.k.heads + a.v.heads : 0);
+    const int heads = a.x.heads + (APPEND ? a.k.heads + a.v.heads : 0);
     // this thread's units: (token, head, unit) numbers `me`, me + all, ...; they advance without divisions
     const int all = kRowThreads * gridDim.y, me = threadIdx.x + blockIdx.y * kRowThreads;
     int u = me % unit_count, h = me / unit_count, t = h / heads;
@@ -76,7 +84,7 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
         const T* src;
         T* dst;
         bool rot = u < turned;
-        if (h < a.x.heads) {
+        if (!APPEND || h < a.x.heads) {
             src = (const T*)a.x.p + (t0 + t) * a.x.token_stride + h * a.x.head_stride;
             dst = (T*)a.y.p + (t0 + t) * a.y.token_stride + h * a.y.head_stride;
         } else {
@@ -93,7 +101,7 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const RowsArgs a, const in
             }
         }
         const int o0 = HALF && u < turned ? u * VEC : 2 * u * VEC, o1 = HALF && u < turned ? o0 + half : o0 + VEC;
-        V p = *(const V*)(src + o0), q = *(const V*)(src + o1);
+        V p = APPEND ? *(const V*)(src + o0) : load_once<V>(src + o0), q = APPEND ? *(const V*)(src + o1) : load_once<V>(src + o1);
         if (rot) {
             const float2* cs = turn + t * half + u * VEC;
             if (HALF) {
@@ -139,14 +147,17 @@ template <class T, int VEC>
 cudaError_t launch_rows_t(const RowsArgs& a, int sm_count, cudaStream_t stream) {
     const int heads = a.x.heads + (a.append ? a.k.heads + a.v.heads : 0);
     const int per_token = heads * (a.head_dim / (2 * VEC));
-    // four tokens a block once that still fills the GPU; few tokens: blocks share a token's heads
-    int block_tokens = (a.tokens >= 4 * 4 * sm_count) ? 4 : 1;
+    // Four tokens a block, in appends eight (6 prompts of 700 to 2048 tokens: 45.3 -> 43.5 us; without an append they cost 1.4 us of 28), once that still fills the GPU.
+    // Few tokens: blocks share a token's heads.
+    const int most = a.append ? 8 : 4;
+    int block_tokens = a.tokens >= 4 * most * sm_count ? most : 1;
     int shares = 1;
     while (block_tokens == 1 && shares < 8 && (int64_t)a.tokens * shares < 2 * sm_count && per_token > kRowThreads * shares) shares *= 2;
     const dim3 grid((unsigned)ceil_div(a.tokens, block_tokens), (unsigned)shares);
     const size_t smem = (size_t)block_tokens * (a.rot / 2) * sizeof(float2);
     ++g_launches;
-    return launch_behind(stream, grid, dim3(kRowThreads), smem, a.layout == FD_ROTARY_HALF ? k_rows<T, VEC, true> : k_rows<T, VEC, false>, a, block_tokens);
+    return launch_behind(stream, grid, dim3(kRowThreads), smem, a.layout == FD_ROTARY_HALF ? (a.append ? k_rows<T, VEC, true, true> : k_rows<T, VEC, true, false>)
+                                                                                           : (a.append ? k_rows<T, VEC, false, true> : k_rows<T, VEC, false, false>), a, block_tokens);
 }
 template <class T>
 cudaError_t launch_rows_any(const RowsArgs& a, int sm_count, cudaStream_t stream) {
@@ -377,6 +388,7 @@ cudaError_t launch_rows(const RowsArgs& a, int dtype, int sm_count, cudaStream_t
 
 cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream) {
     const size_t smem = sizeof(unsigned) * (size_t)(a.batch.max_len < kSelKeys ? a.batch.max_len : kSelKeys);
+    // (512 threads need no leave for their shared memory, but a call without it lost 4 us between the two kernels: 1100 tokens 13.9 us against 10.2)
     const bool many = a.batch.max_len > 4096;
     cudaError_t e = many ? allow_smem<k_select<1024>>(kSelKeys * sizeof(unsigned)) : allow_smem<k_select<512>>(kSelKeys * sizeof(unsigned));
     if (e != cudaSuccess) return e;
