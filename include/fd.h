@@ -446,8 +446,8 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_at
 
 /* Eviction: of every sequence longer than `keep`, each head keeps its first `first` tokens, its last `recent` ones and, of those between, the
  * ones with the largest weights (of equal ones the earlier; a NaN counts as the smallest), `keep` in all and in their order: row r
- * of the new cache is the old slot kept[r].  new_table: the pages they move to, either the same table as the batch's (in place) or pages that
- * no sequence of the batch uses; ceil(keep / page_size) columns suffice.  kept_dev: [batch][heads][keep], -1 behind the last.  new_len_dev:
+ * of the new cache is the old slot kept[r].  new_table: the pages they move to, either the same pages in the same order as the batch's table
+ * (in place; then no other sequence may share them) or pages that no sequence of the batch uses; ceil(keep / page_size) columns suffice.  kept_dev: [batch][heads][keep], -1 behind the last.  new_len_dev:
  * [batch], may be kv_len.  weights_out_dev: the kept weights in their new order, zeros behind them up to kv_len; may be weights_in.
  * q_start is not read. */
 typedef struct {

@@ -311,7 +311,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
     a.out = heads_of(x->out);
     a.heads = d.heads; a.head_dim = d.head_dim; a.dtype = d.dtype;
     a.q_heads = b->total_q > 0 ? x->q.heads : d.heads; a.group = a.q_heads / d.heads; a.tile_tokens = 128 / a.group;
-    a.causal = x->causal ? 1 : 0; a.window = x->window;
+    a.causal = x->causal ? 1 : 0; a.window = std::min(x->window, 1 << 30);       // (no length is above 2^30)
     a.scale_log2 = (float)(x->scale * kLog2e);
     a.lse = x->lse_dev;
     a.w_in = x->weights_in_dev; a.w_out = x->weights_out_dev; a.w_stride = x->weights_stride;

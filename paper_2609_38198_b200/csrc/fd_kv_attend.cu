@@ -739,11 +739,11 @@ template <class T, int D>
 cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
     cudaError_t e = allow_smem<k_attend<T, D>>(Geo<D>::kSmem);
     if (e != cudaSuccess) return e;
-    const int64_t groups = a.batch.total_q / (2 * a.tile_tokens) + std::min(a.batch.batch, a.batch.total_q);
+    const int64_t groups = a.batch.total_q / (2 * a.tile_tokens) + std::min(a.batch.batch, a.batch.total_q), rows = (int64_t)a.batch.total_q * a.q_heads;
+    if (groups * a.heads > INT32_MAX / a.splits || rows > INT32_MAX) return cudaErrorInvalidConfiguration;
     ++g_launches;
     if ((e = launch_behind(stream, dim3((unsigned)(groups * a.heads * a.splits)), dim3(kThreadsAt), Geo<D>::kSmem, k_attend<T, D>, mq, mk, mv, a)) != cudaSuccess) return e;
     if (a.splits == 1) return cudaSuccess;
-    const int64_t rows = (int64_t)a.batch.total_q * a.q_heads;
     ++g_launches;
     if (a.splits > 16) return launch_behind(stream, dim3((unsigned)rows), dim3(256), 0, k_join<T, D, 8>, a);
     return launch_behind(stream, dim3((unsigned)ceil_div(rows, 8)), dim3(256), 0, k_join<T, D, 1>, a);

@@ -321,7 +321,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
         if (*abort_flag) return;
         const int cta0 = cta_of(seg, total, ctas), cta1 = cta_of(seg + units - 1, total, ctas);
         const int64_t slot = 2 * blockIdx.x + ((int)blockIdx.x == cta0 ? 1 : 0);       // a CTA shares its first cache and its last one
-        if ((int)blockIdx.x == cta0 && threadIdx.x == 0) a.parts[b * a.heads + h] = make_int2(cta0, cta1 - cta0 + 1);
+        if ((int)blockIdx.x == cta0 && threadIdx.x == 0) a.parts[(int64_t)b * a.heads + h] = make_int2(cta0, cta1 - cta0 + 1);
         const bool any_odd = *(volatile int*)&flags[1] == segment;
         for (int x = threadIdx.x; x < rows * (D / 4); x += kWarpsFew * 32) {
             const int row = x / (D / 4), d = (x % (D / 4)) * 4;
@@ -377,8 +377,9 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
 }
 
 // Joins the parts of the caches that several CTAs of k_few share: out = sum_p 2^(lse_p - lse) o_p, and turns the scores that k_few left into weights, w_j +=
-// sum over the rows that see token j of 2^(score - lse).  The first `weigh` blocks take 512 tokens of a (sequence, head) each, four a thread; the
-// others a row each, its parts shared by the warps.
+// sum over the rows that see token j of 2^(score - lse).  The first `weigh` blocks, the same number to
+// each (sequence, head), take 512 tokens at a time, four a thread (max_len may lie far above the lengths: no more blocks than keep the GPU busy); the others a
+// row each, its parts shared by the warps.
 constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps, kWeighTokens = 4 * kJoinThreads;
 
 // The parts of a cache: the first CTA that has one and their number (written down by that CTA), and the slot of the p-th.
@@ -387,7 +388,7 @@ struct Parts {
     __device__ __forceinline__ int64_t slot(int p) const { return p == 0 ? 2 * (int64_t)cta0 + 1 : 2 * ((int64_t)cta0 + p); }
 };
 __device__ __forceinline__ Parts few_parts(const AttendArgs& a, int b, int h) {
-    const int2 p = a.parts[b * a.heads + h];
+    const int2 p = a.parts[(int64_t)b * a.heads + h];
     return Parts{p.x, p.y};
 }
 
@@ -400,10 +401,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_few_join(const AttendArgs a, c
     grid_go();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x < weigh) {
-        const int per = (a.batch.max_len + kWeighTokens - 1) / kWeighTokens;
-        const int h = (blockIdx.x / per) % a.heads, key0 = (blockIdx.x % per) * kWeighTokens;
+        const int per = weigh / (a.heads * a.batch.batch), h = (blockIdx.x / per) % a.heads, first = (blockIdx.x % per) * kWeighTokens;
         const Work w = few_work(a, blockIdx.x / (per * a.heads), false);
-        if (key0 >= w.n) return;
+        if (first >= w.n) return;
         const int rows = w.count * a.group;
         if (rows > 0) {
             const Parts parts = few_parts(a, w.b, h);
@@ -426,26 +426,28 @@ __global__ void __launch_bounds__(kJoinThreads) k_few_join(const AttendArgs a, c
             }
         }
         __syncthreads();
-        float sum[4];
-        const int key1 = key0 + threadIdx.x;
-        const float* s = a.scores + ((int64_t)w.b * a.heads + h) * kFewRows * a.score_stride + key1;
+        for (int64_t key0 = first; key0 < w.n; key0 += (int64_t)per * kWeighTokens) {
+            float sum[4];
+            const int key1 = (int)key0 + threadIdx.x;
+            const float* s = a.scores + ((int64_t)w.b * a.heads + h) * kFewRows * a.score_stride + key1;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sum[k] = 0.f;
-        for (int r = 0; r < rows; ++r) {
-            const float lse = s_lse[r];
-            const int lo = s_lo[r], hi = s_hi[r];
+            for (int k = 0; k < 4; ++k) sum[k] = 0.f;
+            for (int r = 0; r < rows; ++r) {
+                const float lse = s_lse[r];
+                const int lo = s_lo[r], hi = s_hi[r];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int key = key1 + kJoinThreads * k;
+                    if (key >= lo && key < hi) sum[k] += ex2f(s[r * a.score_stride + kJoinThreads * k] - lse);
+                }
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int key = key1 + kJoinThreads * k;
-                if (key >= lo && key < hi) sum[k] += ex2f(s[r * a.score_stride + kJoinThreads * k] - lse);
+                if (key >= w.n) continue;
+                const int64_t at = ((int64_t)w.b * a.heads + h) * a.w_stride + key;
+                a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum[k];
             }
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int key = key1 + kJoinThreads * k;
-            if (key >= w.n) continue;
-            const int64_t at = ((int64_t)w.b * a.heads + h) * a.w_stride + key;
-            a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum[k];
         }
         return;
     }
@@ -500,7 +502,9 @@ cudaError_t few_t(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap&
     if (e != cudaSuccess) return e;
     ++g_launches;
     if ((e = launch_behind(stream, dim3((unsigned)a.ctas), dim3(kWarpsFew * 32), GeoFew<D>::kSmem, k_few<T, D>, mk, mv, a)) != cudaSuccess) return e;
-    const int64_t weigh = a.w_out ? ceil_div(a.batch.max_len, kWeighTokens) * a.heads * a.batch.batch : 0, join = a.ctas > 1 ? (int64_t)a.batch.batch * a.heads * a.few_rows : 0;
+    const int64_t caches = (int64_t)a.batch.batch * a.heads, join = a.ctas > 1 ? caches * a.few_rows : 0;
+    const int64_t per = a.w_out ? std::min<int64_t>(ceil_div(a.batch.max_len, kWeighTokens), std::max<int64_t>(1, ceil_div(16 * 148, caches))) : 0, weigh = per * caches;
+    if (weigh + join > INT32_MAX) return cudaErrorInvalidConfiguration;
     if (weigh + join == 0) return cudaSuccess;
     ++g_launches;
     return launch_behind(stream, dim3((unsigned)(weigh + join)), dim3(kJoinThreads), 0, k_few_join<T, D>, a, (int)weigh);

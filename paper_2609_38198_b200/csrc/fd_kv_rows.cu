@@ -39,7 +39,8 @@ __global__ void __launch_bounds__(kRowThreads, APPEND ? 8 : 6) k_rows(const Rows
     using V = Vec<T, VEC>;
     grid_wait();
     grid_go();
-    const int t0 = blockIdx.x * block_tokens, nt = min(block_tokens, a.tokens - t0);
+    const int live = APPEND ? q_begin(a.batch, a.batch.batch) : a.tokens;       // (an append may be padded)
+    const int t0 = blockIdx.x * block_tokens, nt = max(0, min(block_tokens, live - t0));
     const int half = a.rot / 2;
     for (int i = threadIdx.x; i < nt * half; i += kRowThreads) {
         const int t = i / half, f = i - t * half;
@@ -48,7 +49,7 @@ __global__ void __launch_bounds__(kRowThreads, APPEND ? 8 : 6) k_rows(const Rows
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
         turn[i] = make_float2(c * a.scale, s * a.scale * a.sign);
     }
-    if (APPEND && threadIdx.x < nt) {
+    if (APPEND && (int)threadIdx.x < nt) {
         const Batch& B = a.batch;
         const int t = t0 + threadIdx.x;
         int lo = 0, hi = B.batch;                            // last sequence that begins at or before t

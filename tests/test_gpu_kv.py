@@ -232,10 +232,12 @@ def test_append(fd, dtype, dim, page, layout, heads, group, pool_layout):
     k, v, q = (randn(s, T, h, dim, dtype=dtype) for s, h in ((1, heads), (2, heads), (3, heads * group)))
     pos = torch.arange(1000, 1000 + T, dtype=torch.int32, device=DEV)
     freqs = fd.fd_rotary_frequencies(dim // 2, device=DEV)
-    qo = p.cache.append(p.batch, k, v, positions=pos, freqs=freqs, layout=layout, q=q, scale=1.1)
+    qo = torch.full_like(q, 7.0)
+    assert p.cache.append(p.batch, k, v, positions=pos, freqs=freqs, layout=layout, q=q, scale=1.1, q_out=qo) is qo
     p.cache.synchronize()
     want_q = rotate64(q, pos, freqs, layout, 1.1)
-    assert ((qo.double() - want_q).abs() <= rotary_tolerance(q, want_q, freqs, layout, 1.1, dtype)).all()
+    assert ((qo.double() - want_q).abs() <= rotary_tolerance(q, want_q, freqs, layout, 1.1, dtype))[:-2].all()
+    assert (qo[-2:] == 7.0).all(), "rows behind the last sequence"
     t = 0
     turned = fd.fd_rotary(k, pos, freqs, layout=layout, scale=1.1)
     for b, (n, m) in enumerate(zip(kv, new)):
@@ -378,6 +380,50 @@ def test_attend_bad_pages_and_lengths(fd):
             if what == "negative":
                 with pytest.raises(fd.FdError):
                     p.cache.synchronize()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attend_loose_bounds(fd, new):
+    """Bounds far above the lengths (a captured step is sized for the longest context), pages for them, and a window beyond every length."""
+    p = Pool(fd, 5, [300, 1, 2000], [new, 1, new], 2, 64, 16, BF16, cols=20000)
+    q = randn(6, p.total, 8, 64, dtype=BF16)
+    tight, lse, w = check_attend(fd, p, q)
+    loose = fd.KVBatch(p.table, p.kv_len, p.q_start, p.total, new, 300000)
+    wl = torch.zeros(3, 2, 300000, device=DEV)
+    out, lse2 = p.cache.attend(loose, q, weights=wl, window=2 ** 31 - 1)
+    p.cache.synchronize()
+    # (the cache may be cut elsewhere, so sums are taken in another order)
+    assert ((out.double() - tight.double()).abs() <= 2.0 ** -7 * tight.double().abs() + 2.0 ** -9).all() and (lse2 - lse).abs().max() < 1e-5
+    want = torch.zeros_like(wl[:, :, :2003])
+    p.cache.attend(p.batch, q, weights=want)
+    n = p.kv_len.long()[:, None, None]
+    assert ((wl[:, :, :2003] - want).abs() <= 1e-5 * want + 1e-7).all() and (wl[torch.arange(300000, device=DEV).expand_as(wl) >= n] == 0).all()
+
+
+def test_attend_more_new_tokens_than_promised(fd):
+    """max_new chose the kernel for few rows; a sequence with more rows than it holds is left out and reported, the others are answered."""
+    p = Pool(fd, 5, [300, 200], [1, 30], 2, 64, 16, BF16)
+    q = randn(6, 31, 8, 64, dtype=BF16)
+    good, _ = p.cache.attend(p.batch, q)
+    out = torch.full_like(q, 7.0)
+    w = torch.rand(2, 2, 300, device=DEV)
+    w0 = w.clone()
+    p.cache.attend(fd.KVBatch(p.table, p.kv_len, p.q_start, 31, 1, 300), q, out=out, weights=w)
+    with pytest.raises(fd.FdError) as e:
+        p.cache.synchronize()
+    assert e.value.status == fd.FD_ERR_INVALID
+    assert ((out[0].double() - good[0].double()).abs() <= 2.0 ** -7 * good[0].double().abs() + 2.0 ** -9).all()
+    assert (out[1:] == 7.0).all() and torch.equal(w[1], w0[1])
+
+
+@pytest.mark.parametrize("batch", [300, 2000])
+def test_attend_many_sequences(fd, batch):
+    """More sequences than a block has threads, a third of them without a new token, some empty."""
+    rng = np.random.RandomState(batch)
+    kv = [int(x) for x in rng.randint(0, 90, batch)]
+    new = [int(x) for x in rng.randint(0, 3, batch)]
+    p = Pool(fd, 9, kv, new, 1, 64, 8, FP16)
+    check_attend(fd, p, randn(3, p.total, 4, 64, dtype=FP16))
 
 
 def test_attend_refusals(fd):
