@@ -111,7 +111,7 @@ bool same(const fd_heads& a, const fd_heads& b) { return a.p_dev == b.p_dev && a
 }  // namespace
 
 // Few rows a sequence: as many CTAs as the GPU holds at once (two an SM), each with 64 tokens of a cache or more, share the caches evenly.  Else: the cache in parts of
-// at least two tiles of 128, as many as fill the GPU once if every sequence were as long as the longest.
+// at least two tiles of 128, as many as fill the GPU once if every sequence were as long as the longest, none longer than kPartTokens.
 Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weights) {
     Plan p{};
     const int64_t heads = kv->d.heads, group = q_heads / heads, sms = kv->sm_count, live = std::min(b->batch, b->total_q);
@@ -130,7 +130,7 @@ Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weight
         return p;
     }
     const int64_t tiles = std::max<int64_t>(1, ceil_div(b->max_len, 128)), ctas = (b->total_q / (2 * (128 / group)) + live) * heads;
-    const int64_t s = std::max<int64_t>(1, std::min<int64_t>(std::min(sms / ctas, tiles / 2), kMaxSplits));
+    const int64_t s = std::min<int64_t>(std::max<int64_t>({1, std::min(sms / ctas, tiles / 2), ceil_div(b->max_len, kPartTokens)}), kMaxSplits);
     p.split_tiles = (int)ceil_div(tiles, s);
     p.splits = (int)ceil_div(tiles, p.split_tiles);
     if (p.splits > 1) { p.part_o = p.splits * rows * dim; p.part_lse = (p.splits * rows + 3) / 4 * 4; }

@@ -106,6 +106,9 @@ struct AttendArgs {
 // At most this many rows (new tokens x query heads of a group) of a sequence go through the kernel for few rows.
 constexpr int kFewRows = 16;
 constexpr int kMaxSplits = 1024;         // parts of a cache
+// Longest stretch of tokens that one accumulator in tensor memory sums.  The tensor core truncates: of values of one sign, 1e-7 of the sum is lost with every 16
+// tokens (262144 tokens: 1.7e-3, nearly four half steps of fp16); parts are joined with rounding, so the loss ends at 2e-4.
+constexpr int kPartTokens = 32768;
 
 // How the work of a call is cut, and what its workspace holds.
 struct Plan {

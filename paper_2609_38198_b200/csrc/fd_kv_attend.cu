@@ -4,11 +4,18 @@
 // head.  Per tile of 128 cached tokens:
 //   S = Q K^T         (Q in shared memory, K by TMA page by page) into 128 fp32 columns of TMEM;
 //   m, P = 2^(c S - c m)   one thread a row: the maximum over the tile, then exponentials, rounded to the element type and written back over S.
-//                     The maximum in use is raised only when a row exceeds it by 2^8: sums and products stay exact in fp32 (P <= 2^8), and
-//                     the accumulator is read back and rescaled in the first tiles only;
+//                     The maximum in use is raised only when a row exceeds it by 2^8: weights up to 2^8 lose nothing in floating point, and the
+//                     accumulator is read back and rescaled in the first tiles only;
 //   O += P V          (P in TMEM, V row-major in shared memory as an MN-major operand) into D fp32 columns.
 // While one tile's rows are exponentiated the tensor core works on the other's.  Rounding P to 16 bits changes a weight by half an ulp at
 // most, independently per weight; the norm sums the unrounded weights in fp32.
+//
+// Bounds: the tensor core (2 x 1024 clocks for two row tiles of 128 coordinates) and the MUFU (2 x 1024) could be busy all the time; what a pass takes is the chain
+// of one row tile -- scores ready, 600 clocks to read them and find the maximum, 1430 for 128 exponentials of one warp, 950 until the product and the next
+// scores are through -- about 3500 clocks while both row tiles take turns.  8192 new tokens over 16384: 1.56 ms, 1.06 PFLOP/s; without any exponentials 1.36
+// ms (the power limit is near: a library product sustains 1.40 PFLOP/s).  Tried without gain: half a row a thread (16 warps, the maxima
+// exchanged: the same 3880 clocks under the profiler), an eighth of the exponentials as polynomials on the FMA pipe (1.57), a quarter (1.70), weights handed over
+// in one piece (1.64; in four pieces of 32 tokens the product starts on the first).
 //
 // Warps 0-3 / 4-7: softmax of row tile 0 / 1; 8: TMA; 9: MMA; 10, 11: values of tiles that some row sees only in part.  What a row does not see gets P = 0
 // exactly, but 0 x inf = NaN: in those tiles rows behind the sequence are zeroed in shared memory, and so are elements that are not finite; the latter
@@ -25,7 +32,6 @@ namespace {
 using namespace tc;
 
 constexpr int kSoftWarps = 8, kThreadsAt = 32 * (kSoftWarps + 4);
-constexpr int kPolyEvery = 0;            // every so many pairs of exponentials are taken on the FMA pipe; 0: none
 
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
@@ -377,7 +383,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const uint64_t x = fma2(pair2(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), cc, mm);
-                        const uint64_t e = kPolyEvery && i % (kPolyEvery ? kPolyEvery : 1) == kPolyEvery - 1 ? ex2_pair(x) : ex2_mufu(x);
+                        const uint64_t e = ex2_mufu(x);
                         sum[i & 1] = add2(sum[i & 1], e);
                         const float2 v = split2(e);
                         p[i] = Elem<T>::pack(v.x, v.y);
@@ -402,7 +408,9 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         if (ok && t < tiles && warp_on) {
             tc_fence_after();
             const bool empty = m == -INFINITY;
-            const float inv = empty ? 0.f : 1.0f / l;
+            // The tensor core adds with truncation, the norm was summed with rounding: every addition of 16 tokens into the accumulator loses 2.98e-8 of it on average,
+            // which is added back.  (Where all products have one sign it loses 1e-7, for which a cache is cut into parts of kPartTokens.)
+            const float inv = empty ? 0.f : (1.0f + (float)num * (8 * 2.98023224e-8f)) / l;
             const int64_t row = w.begin + token;
             const bool odd = num > 0 && *(volatile int*)&bars->odd;
             if (valid) {

@@ -28,28 +28,6 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-// 2^x of a pair on the FMA pipe, as tc::ex2_fma2, except that a NaN comes through: the power of two is multiplied in instead of being added to the exponent.
-__device__ __forceinline__ uint64_t ex2_pair(uint64_t x) {
-    constexpr float kRound = 12582912.0f;
-    const float2 c = split2(x);
-    x = pair2(max_nan(c.x, -126.0f), max_nan(c.y, -126.0f));
-    const uint64_t t = add2(x, pair2(kRound, kRound));
-    const uint64_t f = sub2(x, add2(t, pair2(-kRound, -kRound)));
-    uint64_t q = pair2(0.00015353363f, 0.00015353363f);
-    q = fma2(q, f, pair2(0.0013398875f, 0.0013398875f));
-    q = fma2(q, f, pair2(0.009618437f, 0.009618437f));
-    q = fma2(q, f, pair2(0.055503324f, 0.055503324f));
-    q = fma2(q, f, pair2(0.24022648f, 0.24022648f));
-    q = fma2(q, f, pair2(0.6931472f, 0.6931472f));
-    q = fma2(q, f, pair2(1.0f, 1.0f));
-    const float2 ts = split2(t);
-    return mul2(q, pair2(__int_as_float((__float_as_int(ts.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(ts.y) << 23) + 0x3f800000)));
-}
 __device__ __forceinline__ uint64_t ex2_mufu(uint64_t x) {
     const float2 c = split2(x);
     return pair2(ex2f(c.x), ex2f(c.y));

@@ -321,6 +321,26 @@ def test_attend_pool_and_tensor_strides(fd):
     assert got is view and torch.equal(view, out) and (wide[..., 128:] == 0).all()
 
 
+def test_attend_long_sums_of_one_sign(fd):
+    """131072 tokens whose values are all positive: truncation in the tensor core's accumulator adds up to no more than a quarter step of fp16 (2^-12) on average.
+    One CTA's accumulator would lose 8e-4."""
+    n, m, heads, dim = 131072, 4096, 8, 64
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k = (torch.randn(n // 64, 64, heads, dim, device=DEV, generator=g) * 0.5).half()
+    v = (1 + torch.rand(dim, device=DEV, generator=g) + 0.1 * torch.rand(n // 64, 64, heads, dim, device=DEV, generator=g)).half()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    cache = fd.KVCache(k, v)
+    batch = fd.KVBatch(torch.arange(n // 64, dtype=torch.int32, device=DEV)[None], i32(n), i32(0, m), m, m, n)
+    q = torch.randn(m, heads, dim, device=DEV, generator=g).half()
+    out, lse = cache.attend(batch, q, causal=False)
+    cache.synchronize()
+    for h in (0, heads - 1):
+        s = q[:64, h].double() @ k[:, :, h].reshape(n, dim).double().T / 8
+        want = torch.softmax(s, -1) @ v[:, :, h].reshape(n, dim).double()
+        assert abs(float((out[:64, h].double() / want - 1).mean())) <= 2.0 ** -12
+        assert (lse[:64, h].double() - torch.logsumexp(s, -1)).abs().max() < 1e-5
+
+
 def test_attend_far_offsets(fd):
     """A pool of more than 2^32 bytes and 2^31 elements a tensor: pages at its end."""
     pages, page, heads, dim = 70000, 32, 8, 128              # 2.3e9 elements
@@ -568,6 +588,28 @@ def test_evict(fd, kind, keep, first, recent, in_place):
             have = w_new[b, h].cpu().numpy()
             assert np.array_equal(have[:m], w[b, h, want], equal_nan=True) and (have[m:n] == 0).all()
             assert np.array_equal(have[n:], w[b, h, n:] if in_place else np.full(3001 - n, 5.0, np.float32), equal_nan=True)
+
+
+@pytest.mark.parametrize("kind", ["random", "ties"])
+def test_evict_long(fd, kind):
+    """Beyond what a block keeps in shared memory (40960 tokens), and beyond 4096 (more threads)."""
+    kv, keep = [45000, 5000, 41500], 3000
+    p = Pool(fd, 17, kv, [0] * 3, 1, 64, 64, BF16)
+    w = np.random.RandomState(4).rand(3, 1, 45000).astype(np.float32)
+    if kind == "ties":
+        w = np.floor(w * 3).astype(np.float32)
+    wd = torch.from_numpy(w).to(DEV)
+    old = [p.rows(b) for b in range(3)]
+    kept, n, w_new = p.cache.evict(p.batch, wd, keep, first=7, recent=300)
+    p.cache.synchronize()
+    assert n.tolist() == [keep] * 3
+    for b in range(3):
+        want = evict_plain(w[b, 0, :kv[b]], kv[b], keep, 7, 300)
+        assert kept[b, 0].tolist() == want.tolist()
+        now = p.rows(b, keep)
+        src = torch.from_numpy(want).to(DEV)
+        assert torch.equal(now[0], old[b][0][src]) and torch.equal(now[1], old[b][1][src])
+        assert np.array_equal(w_new[b, 0, :keep].cpu().numpy(), w[b, 0, want]) and (w_new[b, 0, keep:kv[b]] == 0).all()
 
 
 def test_decode_with_eviction(fd):
