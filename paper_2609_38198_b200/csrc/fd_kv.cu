@@ -88,7 +88,9 @@ fd_status check_batch(const Err& err, const fd_kv* kv, const fd_kv_batch* b, boo
     return FD_OK;
 }
 Batch batch_of(const fd_kv* kv, const fd_kv_batch* b) {
-    return Batch{b->table_dev, b->table_stride, b->kv_len_dev, b->q_start_dev, b->batch, b->max_pages, b->total_q, b->max_len, kv->d.page_size, kv->d.num_pages, kv->d.status_dev};
+    const int p = kv->d.page_size;
+    return Batch{b->table_dev, b->table_stride, b->kv_len_dev, b->q_start_dev, b->batch, b->max_pages, b->total_q, b->max_len, p, kv->d.num_pages,
+                 (p & (p - 1)) ? -1 : __builtin_ctz(p), kv->d.status_dev};
 }
 fd_status check_device(const Err& err, const fd_kv* kv) {
     int dev = -1;

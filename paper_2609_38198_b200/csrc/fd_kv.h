@@ -43,7 +43,11 @@ struct Batch {
     const int* table; int64_t table_stride;
     const int* kv_len; const int* q_start;
     int batch, max_pages, total_q, max_len, page_size, num_pages;
+    int page_shift;                  // log2(page_size), or -1: moving rows spends most of its instructions on divisions otherwise
     unsigned int* status;
+    // Page of a slot and the slot's row in it.
+    __device__ __forceinline__ int page_of(int slot) const { return page_shift >= 0 ? slot >> page_shift : slot / page_size; }
+    __device__ __forceinline__ int row_of(int slot) const { return page_shift >= 0 ? slot & (page_size - 1) : slot % page_size; }
 };
 
 // Sequence b's tokens in the cache, never more than its row of the page table holds.

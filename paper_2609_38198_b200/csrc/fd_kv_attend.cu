@@ -125,7 +125,7 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
     const bool mine = lane < boxes && key < w.n;
     int page = 0;
     if (mine) {
-        page = a.batch.table[w.b * a.batch.table_stride + key / a.batch.page_size];
+        page = a.batch.table[w.b * a.batch.table_stride + a.batch.page_of(key)];
         if (page < 0 || page >= a.batch.num_pages) { page = a.batch.num_pages; atomicOr(a.batch.status, kBadPage); }   // (outside: TMA fills with zeros)
     }
     const int total = __popc(__ballot_sync(~0u, mine));
@@ -134,7 +134,7 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
     if (mine)
 #pragma unroll
         for (int c = 0; c < Geo<D>::kChunks; ++c)
-            tma_load_4d(dst + c * Geo<D>::kChunkBytes + lane * a.box_rows * 128, map, c * 64, key % a.batch.page_size, h, page, bar);
+            tma_load_4d(dst + c * Geo<D>::kChunkBytes + lane * a.box_rows * 128, map, c * 64, a.batch.row_of(key), h, page, bar);
     __syncwarp();
 }
 
@@ -429,9 +429,9 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     // what is not finite in tiles that this CTA's rows see in part, for the rows that see it
                     for (int key = max(lo, j0 * 128); key < min(hi, j1 * 128); ++key) {
                         if (key / 128 >= full0 && key / 128 < full1) { key = full1 * 128 - 1; continue; }
-                        const int page = a.batch.table[w.b * a.batch.table_stride + key / a.batch.page_size];
+                        const int page = a.batch.table[w.b * a.batch.table_stride + a.batch.page_of(key)];
                         if (page < 0 || page >= a.batch.num_pages) continue;
-                        const int64_t at = page * a.v_page + (key % a.batch.page_size) * a.v_token + h * a.v_head + d0;
+                        const int64_t at = page * a.v_page + a.batch.row_of(key) * a.v_token + h * a.v_head + d0;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const float v = Elem<T>::at(a.v_pool, at + i);

@@ -161,7 +161,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                 const int ii = (e + lane) / boxes, key = (c0 + warp + kWarpsFew * ii) * KEYS + ((e + lane) % boxes) * a.box_rows;
                 page = 0;
                 if (ii < mine && key < w.n) {
-                    page = a.batch.table[b * a.batch.table_stride + key / a.batch.page_size];
+                    page = a.batch.table[b * a.batch.table_stride + a.batch.page_of(key)];
                     if (page < 0 || page >= a.batch.num_pages) { page = a.batch.num_pages; atomicOr(a.batch.status, kBadPage); }   // (outside: TMA fills with zeros)
                 }
             }
@@ -174,8 +174,8 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
             if (lane < live) {
 #pragma unroll
                 for (int x = 0; x < D / 64; ++x) {
-                    tma_load_4d(k + x * G::kHalf + lane * a.box_rows * 128, &map_k, x * 64, key % a.batch.page_size, h, at, &full[st]);
-                    tma_load_4d(k + G::kTile + x * G::kHalf + lane * a.box_rows * 128, &map_v, x * 64, key % a.batch.page_size, h, at, &full[st]);
+                    tma_load_4d(k + x * G::kHalf + lane * a.box_rows * 128, &map_k, x * 64, a.batch.row_of(key), h, at, &full[st]);
+                    tma_load_4d(k + G::kTile + x * G::kHalf + lane * a.box_rows * 128, &map_v, x * 64, a.batch.row_of(key), h, at, &full[st]);
                 }
             }
             __syncwarp();
@@ -350,9 +350,9 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                 for (int key = max(see_lo(a, w, token), k0); key < min(see_hi(a, w, token), k1); ++key) {
                     const int chunk = key / KEYS * KEYS;
                     if (chunk >= full0 && chunk + KEYS <= full1) continue;
-                    const int page = a.batch.table[b * a.batch.table_stride + key / a.batch.page_size];
+                    const int page = a.batch.table[b * a.batch.table_stride + a.batch.page_of(key)];
                     if (page < 0 || page >= a.batch.num_pages) continue;
-                    const int64_t from = page * a.v_page + (key % a.batch.page_size) * a.v_token + h * a.v_head + d;
+                    const int64_t from = page * a.v_page + a.batch.row_of(key) * a.v_token + h * a.v_head + d;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float y = Elem<T>::at(a.v_pool, from + e);

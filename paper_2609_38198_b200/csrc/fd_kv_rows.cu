@@ -61,12 +61,12 @@ __global__ void __launch_bounds__(kRowThreads, APPEND ? 8 : 6) k_rows(const Rows
         place[threadIdx.x][0] = place[threadIdx.x][1] = -1;
         if (t >= begin && t < end) {
             const int n = kv_length(B, lo, true), slot = n - (end - begin) + (t - begin);
-            const int page = slot < 0 ? -1 : B.table[lo * B.table_stride + slot / B.page_size];
+            const int page = slot < 0 ? -1 : B.table[lo * B.table_stride + B.page_of(slot)];
             if (slot < 0) atomicOr(B.status, kBadLength);
             else if (page < 0 || page >= B.num_pages) atomicOr(B.status, kBadPage);
             else {
-                place[threadIdx.x][0] = page * a.k_page + (slot % B.page_size) * a.k_token;
-                place[threadIdx.x][1] = page * a.v_page + (slot % B.page_size) * a.v_token;
+                place[threadIdx.x][0] = page * a.k_page + B.row_of(slot) * a.k_token;
+                place[threadIdx.x][1] = page * a.v_page + B.row_of(slot) * a.v_token;
             }
         }
     }
@@ -294,8 +294,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, uint16_t* pool, in
 #pragma unroll
         for (int u = 0; u < kMoveDepth; ++u) {
             const int r = r0 + u * kRows + mine;
-            pf[u] = s[u] >= 0 ? from[s[u] / B.page_size] : 0;
-            pt[u] = s[u] >= 0 ? to[r / B.page_size] : 0;
+            pf[u] = s[u] >= 0 ? from[B.page_of(s[u])] : 0;
+            pt[u] = s[u] >= 0 ? to[B.page_of(r)] : 0;
         }
     };
     slots(r0, slot[0]);
@@ -308,8 +308,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, uint16_t* pool, in
 #pragma unroll
         for (int u = 0; u < kMoveDepth; ++u) {
             const int r = r0 + u * kRows + mine, s = slot[0][u];
-            const int64_t src = pf[u] * page_s + (s % B.page_size) * token_s;
-            dst[u] = pt[u] * page_s + (r % B.page_size) * token_s;
+            const int64_t src = pf[u] * page_s + B.row_of(s) * token_s;
+            dst[u] = pt[u] * page_s + B.row_of(r) * token_s;
             const bool off = pf[u] < 0 || pf[u] >= B.num_pages || pt[u] < 0 || pt[u] >= B.num_pages;
             bad |= off;
             if (s < 0 || off || src == dst[u]) dst[u] = -1;
