@@ -131,8 +131,10 @@ Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weight
         }
         return p;
     }
-    const int64_t tiles = std::max<int64_t>(1, ceil_div(b->max_len, 128)), ctas = (b->total_q / (2 * (128 / group)) + live) * heads;
-    const int64_t s = std::min<int64_t>(std::max<int64_t>({1, std::min(sms / ctas, tiles / 2), ceil_div(b->max_len, kPartTokens)}), kMaxSplits);
+    p.row_tiles = b->max_new <= 128 / group ? 1 : 2;
+    const int64_t tiles = std::max<int64_t>(1, ceil_div(b->max_len, 128));
+    const int64_t ctas = p.row_tiles == 1 ? live * heads : (b->total_q / (2 * (128 / group)) + live) * heads, room = p.row_tiles == 1 ? 2 * sms : sms;
+    const int64_t s = std::min<int64_t>(std::max<int64_t>({1, std::min(room / ctas, tiles / 2), ceil_div(b->max_len, kPartTokens)}), kMaxSplits);
     p.split_tiles = (int)ceil_div(tiles, s);
     p.splits = (int)ceil_div(tiles, p.split_tiles);
     if (p.splits > 1) { p.part_o = p.splits * rows * dim; p.part_lse = (p.splits * rows + 3) / 4 * 4; }
@@ -328,7 +330,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
         if (need && (!workspace_dev || workspace_bytes < need)) return err(FD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
         if (need && (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return err(FD_ERR_INVALID, "workspace must be 16-byte aligned");
         few = p.few;
-        a.splits = p.splits; a.split_tiles = p.split_tiles; a.ctas = p.ctas; a.few_rows = b->max_new * a.group;
+        a.row_tiles = p.row_tiles; a.splits = p.splits; a.split_tiles = p.split_tiles; a.ctas = p.ctas; a.few_rows = b->max_new * a.group;
         a.parts = static_cast<int2*>(workspace_dev);
         a.part_o = static_cast<float*>(workspace_dev) + p.parts;
         a.part_lse = a.part_o + p.part_o;

@@ -99,6 +99,7 @@ struct AttendArgs {
     float scale_log2;                // scale * log2(e)
     float* lse;
     const float* w_in; float* w_out; int64_t w_stride;
+    int row_tiles;                   // many rows: tiles of 128 rows a CTA
     int splits, split_tiles;         // many rows: the cache in `splits` parts of split_tiles tiles of 128 tokens
     int ctas, few_rows;              // few rows: CTAs that share the batch's caches; rows a sequence has at most; first CTA and number of the parts of each
     int2* parts;                     // (sequence, head)
@@ -117,7 +118,7 @@ constexpr int kPartTokens = 32768;
 // How the work of a call is cut, and what its workspace holds.
 struct Plan {
     bool few;
-    int splits, split_tiles, ctas;
+    int row_tiles, splits, split_tiles, ctas;
     int64_t score_stride;
     size_t parts, part_o, part_lse, scores;         // in floats, in this order, each a multiple of 4
     size_t bytes() const { return (parts + part_o + part_lse + scores) * sizeof(float); }

@@ -1,6 +1,6 @@
 // Attention of new tokens over a paged cache, and its column sums, on tcgen05 / TMEM.
 //
-// k_attend.  One CTA takes two tiles of 128 rows; a row is a (new token, query head of the group), so that all rows of a tile read the same cached
+// k_attend.  One CTA takes two tiles of 128 rows (one, where no sequence has more: then two CTAs share an SM); a row is a (new token, query head of the group), so that all rows of a tile read the same cached
 // head.  Per tile of 128 cached tokens:
 //   S = Q K^T         (Q in shared memory, K by TMA page by page) into 128 fp32 columns of TMEM;
 //   m, P = 2^(c S - c m)   one thread a row: the maximum over the tile, then exponentials, rounded to the element type and written back over S.
@@ -30,8 +30,6 @@ namespace kv {
 namespace {
 
 using namespace tc;
-
-constexpr int kSoftWarps = 8, kThreadsAt = 32 * (kSoftWarps + 4);
 
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
@@ -70,15 +68,21 @@ struct Geo {
     static constexpr int kChunks = D / 64;                     // 128-byte columns of an operand tile
     static constexpr int kChunkBytes = 128 * 128;              // 128 rows of one
     static constexpr int kTile = kChunks * kChunkBytes;
-    static constexpr int kSlots = D == 128 ? 5 : 8;            // ring of key and value tiles
-    static constexpr int kSmem = 1024 + (2 + kSlots) * kTile + 512;
+};
+// A CTA's row tiles: two, or one where no sequence has more rows and the cache's bytes count; then two CTAs an SM fill each other's waits (5 new tokens of 8 sequences of
+// 6000 to 16384, 64 query heads on 8: 157 -> 116 us; 2 tokens of 24 sequences of 1400 to 4096, 64 coordinates: 59 -> 35 us).
+template <int D, int TILES>
+struct GeoAt {
+    static constexpr int kSlots = TILES == 2 ? (D == 128 ? 5 : 8) : (D == 128 ? 2 : 4);        // ring of key and value tiles
+    static constexpr int kSmem = 1024 + (TILES + kSlots) * Geo<D>::kTile + 512;
+    static constexpr int kSoftWarps = 4 * TILES, kThreads = 32 * (kSoftWarps + 4), kCols = 256 * TILES;
     // Key and value tiles take turns in the ring; the j-th value tile is use number value_use(j) of its slot by values.
     static __device__ __forceinline__ int value_use(int j) { return j / (kSlots % 2 ? kSlots : kSlots / 2); }
 };
 
-template <int D>
+template <int SLOTS>
 struct Bars {
-    uint64_t q_full, full[Geo<D>::kSlots], empty[Geo<D>::kSlots], clean[Geo<D>::kSlots];
+    uint64_t q_full, full[SLOTS], empty[SLOTS], clean[SLOTS];
     uint64_t s_full[2], p_full[2][4], pv_done[2];
     uint32_t tmem_base;
     int abort_flag, odd;                                        // odd: elements that are not finite were taken out of a tile
@@ -138,16 +142,18 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
     __syncwarp();
 }
 
-template <class T, int D>
-__global__ void __launch_bounds__(kThreadsAt, 1)
+template <class T, int D, int TILES>
+__global__ void __launch_bounds__(GeoAt<D, TILES>::kThreads, TILES == 2 ? 1 : 2)
 k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
          const AttendArgs a) {
     using G = Geo<D>;
+    using A = GeoAt<D, TILES>;
+    constexpr int kSoftWarps = A::kSoftWarps;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* base = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* q_base = base;
-    uint8_t* ring = base + 2 * G::kTile;
-    Bars<D>* bars = (Bars<D>*)(ring + G::kSlots * G::kTile);
+    uint8_t* ring = base + TILES * G::kTile;
+    Bars<A::kSlots>* bars = (Bars<A::kSlots>*)(ring + A::kSlots * G::kTile);
     volatile int* abort_flag = &bars->abort_flag;
     unsigned int* status = a.batch.status + 1;
 
@@ -156,11 +162,11 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     // work items: split fastest, then head, then token group, the last groups (which see most) first
     const int split = blockIdx.x % a.splits, h = (blockIdx.x / a.splits) % a.heads;
     const int groups = gridDim.x / (a.splits * a.heads), slot = groups - 1 - blockIdx.x / (a.splits * a.heads);
-    const int per = 2 * a.tile_tokens;
+    const int per = TILES * a.tile_tokens;
     const Work w = uniform(find_work(a.batch, slot, per));
     if (w.b < 0) return;
     const int t_last = min(w.count, w.t0 + per) - 1;
-    const int tiles = (t_last - w.t0) / a.tile_tokens + 1;               // row tiles with work: 1 or 2
+    const int tiles = (t_last - w.t0) / a.tile_tokens + 1;               // row tiles with work
     int j0 = see_lo(a, w, w.t0) / 128, j1 = (see_hi(a, w, t_last) + 127) / 128;
     if (a.splits > 1) { j0 = max(j0, split * a.split_tiles); j1 = min(j1, (split + 1) * a.split_tiles); }
     const int num = max(0, j1 - j0);
@@ -170,7 +176,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     const int warp = warp_index(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         mbar_init(&bars->q_full, 1);
-        for (int s = 0; s < G::kSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); mbar_init(&bars->clean[s], 2); }
+        for (int s = 0; s < A::kSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); mbar_init(&bars->clean[s], 2); }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&bars->s_full[t], 1); mbar_init(&bars->pv_done[t], 1);
             for (int k = 0; k < 4; ++k) mbar_init(&bars->p_full[t][k], 4);
@@ -179,7 +185,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kSoftWarps) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(A::kCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -201,16 +207,16 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             bool ok = true;
             int it = 0;
             for (; it < 2 * num; ++it) {
-                const int s = it % G::kSlots;
-                ok = mbar_wait(&bars->empty[s], ((it / G::kSlots) & 1) ^ 1, abort_flag, status, 1);
+                const int s = it % A::kSlots;
+                ok = mbar_wait(&bars->empty[s], ((it / A::kSlots) & 1) ^ 1, abort_flag, status, 1);
                 ok = __all_sync(~0u, ok);
                 if (!ok) break;
                 load_tile<D>(ring + s * G::kTile, (it & 1) ? &map_v : &map_k, a, w, j0 + it / 2, h, &bars->full[s]);
             }
             if (!ok && lane == 0) {             // aborted: copies in flight land before the CTA exits (bounded)
-                for (int k = max(0, it - G::kSlots); k < it; ++k) {
+                for (int k = max(0, it - A::kSlots); k < it; ++k) {
                     const long long c0 = clock64();
-                    while (!mbar_try_wait(&bars->full[k % G::kSlots], (k / G::kSlots) & 1) && clock64() - c0 < 20000000ll) {}
+                    while (!mbar_try_wait(&bars->full[k % A::kSlots], (k / A::kSlots) & 1) && clock64() - c0 < 20000000ll) {}
                 }
                 const long long c0 = clock64();
                 while (!mbar_try_wait(&bars->q_full, 0) && clock64() - c0 < 20000000ll) {}
@@ -241,11 +247,11 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     tc_commit(&bars->empty[0]);
                 }
                 for (int j = 0; j < num && ok; ++j) {
-                    const int iv = 2 * j + 1, sv = iv % G::kSlots, ik = 2 * j + 2, sk = ik % G::kSlots;
-                    ok = mbar_wait(&bars->full[sv], (iv / G::kSlots) & 1, abort_flag, status, 4) &&
-                         mbar_wait(&bars->clean[sv], G::value_use(j) & 1, abort_flag, status, 5);
+                    const int iv = 2 * j + 1, sv = iv % A::kSlots, ik = 2 * j + 2, sk = ik % A::kSlots;
+                    ok = mbar_wait(&bars->full[sv], (iv / A::kSlots) & 1, abort_flag, status, 4) &&
+                         mbar_wait(&bars->clean[sv], A::value_use(j) & 1, abort_flag, status, 5);
                     for (int t = 0; t < tiles && ok; ++t) {
-                        const uint32_t o_addr = tmem + 256u + (uint32_t)D * t, p_addr = tmem + 128u * t, vt = v_lo + (uint32_t)(sv * G::kTile >> 4);
+                        const uint32_t o_addr = tmem + 128u * TILES + (uint32_t)D * t, p_addr = tmem + 128u * t, vt = v_lo + (uint32_t)(sv * G::kTile >> 4);
 #pragma unroll
                         for (int part = 0; part < 4; ++part) {                  // 32 tokens each
                             ok = mbar_wait_near(&bars->p_full[t][part], j & 1, abort_flag, status, 6);
@@ -261,7 +267,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         tc_commit(&bars->pv_done[t]);
                         if (j + 1 < num) {
                             if (t == 0) {
-                                ok = mbar_wait(&bars->full[sk], (ik / G::kSlots) & 1, abort_flag, status, 7);
+                                ok = mbar_wait(&bars->full[sk], (ik / A::kSlots) & 1, abort_flag, status, 7);
                                 if (!ok) break;
                                 tc_fence_after();
                             }
@@ -277,8 +283,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             // ---------------------------------------------------------------- values that some row does not see
             bool ok = true;
             for (int j = 0; j < num; ++j) {
-                const int iv = 2 * j + 1, sv = iv % G::kSlots, tile = j0 + j;
-                ok = __all_sync(~0u, mbar_wait(&bars->full[sv], (iv / G::kSlots) & 1, abort_flag, status, 8));
+                const int iv = 2 * j + 1, sv = iv % A::kSlots, tile = j0 + j;
+                ok = __all_sync(~0u, mbar_wait(&bars->full[sv], (iv / A::kSlots) & 1, abort_flag, status, 8));
                 if (!ok) break;
                 if (tile < full0 || tile >= full1) {
                     uint8_t* v = ring + sv * G::kTile;
@@ -308,7 +314,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         // -------------------------------------------------------------------- softmax (thread = row)
         const int t = warp >> 2, q = warp & 3, r = q * 32 + lane;
         const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
-        const uint32_t s_addr = tmem + lane_addr + 128u * t, o_addr = tmem + lane_addr + 256u + (uint32_t)D * t;
+        const uint32_t s_addr = tmem + lane_addr + 128u * t, o_addr = tmem + lane_addr + 128u * TILES + (uint32_t)D * t;
         const int token = w.t0 + t * a.tile_tokens + r / a.group, head = h * a.group + r % a.group;
         const bool valid = r < a.tile_tokens * a.group && token < w.count;
         const bool warp_on = __any_sync(~0u, valid);                     // warps without rows only keep the hand-offs going
@@ -326,29 +332,40 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     continue;
                 }
                 tc_fence_after();
-                uint32_t s[4][32];
+                // One row tile: two CTAs share the registers, so the scores are read twice, 32 tokens at a time; two row tiles: once (read twice they take 2.5 % longer).
+                constexpr bool kHold = TILES == 2;
+                uint32_t s[kHold ? 4 : 2][32];
                 float mx[4];
-                tmem_ld32(s_addr, s[0]);
-                tmem_ld32(s_addr + 32, s[1]);
-                tmem_wait_ld();
-                tmem_ld32(s_addr + 64, s[2]);
-                tmem_ld32(s_addr + 96, s[3]);
                 const bool whole = tile >= full0 && tile < full1;
+                auto hide = [&](int k, uint32_t (&x)[32]) {              // what the row does not see
+                    if (whole) return;
+                    const uint32_t see = col_mask(lo, hi, tile * 128 + 32 * k);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!((see >> i) & 1)) x[i] = 0xff800000u;
+                };
+                tmem_ld32(s_addr, s[0]);
+                if (kHold) {
+                    tmem_ld32(s_addr + 32, s[1]);
+                    tmem_wait_ld();
+                    tmem_ld32(s_addr + 64, s[kHold ? 2 : 0]);
+                    tmem_ld32(s_addr + 96, s[kHold ? 3 : 0]);
+                }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    if (k == 2) tmem_wait_ld();
-                    if (!whole) {
-                        const uint32_t see = col_mask(lo, hi, tile * 128 + 32 * k);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!((see >> i) & 1)) s[k][i] = 0xff800000u;
+                    uint32_t (&x)[32] = s[kHold ? k : k % 2];
+                    if (kHold && k == 2) tmem_wait_ld();
+                    if (!kHold) {
+                        tmem_wait_ld();
+                        if (k < 3) tmem_ld32(s_addr + 32 * (k + 1), s[(k + 1) % 2]);
                     }
+                    hide(k, x);
                     float y[2];
 #pragma unroll
                     for (int z = 0; z < 2; ++z) {
-                        y[z] = max_nan(__uint_as_float(s[k][16 * z]), __uint_as_float(s[k][16 * z + 1]));
+                        y[z] = max_nan(__uint_as_float(x[16 * z]), __uint_as_float(x[16 * z + 1]));
 #pragma unroll
-                        for (int i = 2; i < 16; i += 2) y[z] = max_nan(y[z], __uint_as_float(s[k][16 * z + i]), __uint_as_float(s[k][16 * z + i + 1]));
+                        for (int i = 2; i < 16; i += 2) y[z] = max_nan(y[z], __uint_as_float(x[16 * z + i]), __uint_as_float(x[16 * z + i + 1]));
                     }
                     mx[k] = max_nan(y[0], y[1]);
                 }
@@ -376,13 +393,20 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 const float mc = m == -INFINITY ? 0.f : m * c;
                 const uint64_t cc = pair2(c, c), mm = pair2(-mc, -mc);
                 uint64_t sum[2] = {0, 0};
+                if (!kHold) tmem_ld32(s_addr, s[0]);
                 // 32 tokens at a time: the store of one part completes while the next part's exponentials are taken, then the product may have it
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
+                    uint32_t (&sk)[32] = s[kHold ? k : k % 2];
+                    if (!kHold) {
+                        tmem_wait_ld();
+                        if (k < 3) tmem_ld32(s_addr + 32 * (k + 1), s[(k + 1) % 2]);
+                        hide(k, sk);
+                    }
                     uint32_t p[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const uint64_t x = fma2(pair2(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), cc, mm);
+                        const uint64_t x = fma2(pair2(__uint_as_float(sk[2 * i]), __uint_as_float(sk[2 * i + 1])), cc, mm);
                         const uint64_t e = ex2_mufu(x);
                         sum[i & 1] = add2(sum[i & 1], e);
                         const float2 v = split2(e);
@@ -458,7 +482,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     tc_fence_before();
     __syncthreads();
     if (warp == kSoftWarps) {
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(A::kCols) : "memory");
     }
 }
 
@@ -743,15 +767,22 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     }
 }
 
+template <class T, int D, int TILES>
+cudaError_t launch_tiles(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
+    using A = GeoAt<D, TILES>;
+    const cudaError_t e = allow_smem<k_attend<T, D, TILES>>(A::kSmem);
+    if (e != cudaSuccess) return e;
+    const int64_t groups = a.batch.total_q / (TILES * a.tile_tokens) + std::min(a.batch.batch, a.batch.total_q);
+    if (groups * a.heads > INT32_MAX / a.splits) return cudaErrorInvalidConfiguration;
+    ++g_launches;
+    return launch_behind(stream, dim3((unsigned)(groups * a.heads * a.splits)), dim3(A::kThreads), A::kSmem, k_attend<T, D, TILES>, mq, mk, mv, a);
+}
 template <class T, int D>
 cudaError_t attend_t(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
-    cudaError_t e = allow_smem<k_attend<T, D>>(Geo<D>::kSmem);
-    if (e != cudaSuccess) return e;
-    const int64_t groups = a.batch.total_q / (2 * a.tile_tokens) + std::min(a.batch.batch, a.batch.total_q), rows = (int64_t)a.batch.total_q * a.q_heads;
-    if (groups * a.heads > INT32_MAX / a.splits || rows > INT32_MAX) return cudaErrorInvalidConfiguration;
-    ++g_launches;
-    if ((e = launch_behind(stream, dim3((unsigned)(groups * a.heads * a.splits)), dim3(kThreadsAt), Geo<D>::kSmem, k_attend<T, D>, mq, mk, mv, a)) != cudaSuccess) return e;
-    if (a.splits == 1) return cudaSuccess;
+    const int64_t rows = (int64_t)a.batch.total_q * a.q_heads;
+    if (rows > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const cudaError_t e = a.row_tiles == 1 ? launch_tiles<T, D, 1>(a, mq, mk, mv, stream) : launch_tiles<T, D, 2>(a, mq, mk, mv, stream);
+    if (e != cudaSuccess || a.splits == 1) return e;
     ++g_launches;
     if (a.splits > 16) return launch_behind(stream, dim3((unsigned)rows), dim3(256), 0, k_join<T, D, 8>, a);
     return launch_behind(stream, dim3((unsigned)ceil_div(rows, 8)), dim3(256), 0, k_join<T, D, 1>, a);
