@@ -388,8 +388,10 @@ struct Parts {
     __device__ __forceinline__ int64_t slot(int p) const { return p == 0 ? 2 * (int64_t)cta0 + 1 : 2 * ((int64_t)cta0 + p); }
 };
 __device__ __forceinline__ Parts few_parts(const AttendArgs& a, int b, int h) {
+    // (held to what there is: a CTA that gave up in a bounded wait has written nothing)
     const int2 p = a.parts[(int64_t)b * a.heads + h];
-    return Parts{p.x, p.y};
+    const int c0 = min(max(p.x, 0), a.ctas - 1);
+    return Parts{c0, min(max(p.y, 1), a.ctas - c0)};
 }
 
 template <class T, int D>
