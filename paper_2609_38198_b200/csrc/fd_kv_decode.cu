@@ -362,8 +362,9 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
             }
             const float lse2 = top == -INFINITY ? -INFINITY : top * c + log2f(sum);
             if (cta0 != cta1) {
+                // (zeros, where the row sees nothing of the part: the join multiplies every part's result by a factor, which is 0 there)
                 if (d == 0) a.part_lse[slot * kFewRows + row] = lse2;
-                if (top != -INFINITY) *(float4*)(a.part_o + (slot * kFewRows + row) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+                *(float4*)(a.part_o + (slot * kFewRows + row) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
             } else {
                 *(uint2*)((T*)a.out.p + at * a.out.token_stride + head * a.out.head_stride + d) = make_uint2(Elem<T>::pack(v[0], v[1]), Elem<T>::pack(v[2], v[3]));
                 if (d == 0 && a.lse) a.lse[at * a.q_heads + head] = lse2 == -INFINITY ? -INFINITY : (float)((double)lse2 * 0.69314718055994530942);

@@ -675,3 +675,44 @@ def test_attend_against_the_kernel_product(fd):
     _, _, _, tol, _ = attend64(p, q, 2 * beta, causal=False)
     assert float((out[:, 0].double() - want).norm()) <= float(tol.norm()) + 2e-5 * float(want.norm())
     ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------ workspaces, bounds, aliases
+def attend_raw(pool, q, out, lse, fill=0xFF, causal=True, window=0, w_in=None, w_out=None, scale=None):
+    """The C entry point with a workspace whose every byte is `fill` (0xFF: NaN)."""
+    import ctypes
+    from paper_2609_38198_b200 import binding as b
+    head = lambda t: b.fd_heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1])  # noqa: E731
+    ptr = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
+    a = b.fd_kv_attend_args(head(q), head(out), pool.dim ** -0.5 if scale is None else scale, int(causal), window, ptr(lse), ptr(w_in), ptr(w_out),
+                            0 if w_out is None else w_out.shape[2])
+    ref = ctypes.byref(pool.batch.struct)
+    size = b.lib.fd_kv_attend_bytes(pool.cache._h, ref, q.shape[1], 0 if w_out is None else 1)
+    ws = torch.full((max(size, 16),), fill, dtype=torch.uint8, device=DEV)
+    err = ctypes.create_string_buffer(256)
+    st = b.lib.fd_kv_attend(pool.cache._h, ref, ctypes.byref(a), ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream, err, 256)
+    assert st == 0, err.value
+    pool.cache.synchronize()
+    return size
+
+
+@pytest.mark.parametrize("dtype,dim", [(BF16, 128), (FP16, 64)])
+@pytest.mark.parametrize("new,group", [(2, 1), (5, 3), (4, 4), (30, 2)])
+@pytest.mark.parametrize("mask", ["causal", "window 65", "window 130", "window 600"])
+def test_attend_workspace_of_any_content(fd, dtype, dim, new, group, mask):
+    """Nothing of the workspace is used that the call has not written: parts of a cache that one of several new tokens does not see, at the end of the cache
+    (causal) and at the front of a window."""
+    window = int(mask.split()[1]) if mask.startswith("window") else 0
+    for n in (65, 66, 67, 68, 705, 709, 4099):
+        p = Pool(fd, n + new, [n], [min(new, n)], 2, dim, 16, dtype)
+        q = randn(n, p.total, 2 * group, dim, dtype=dtype, scale=2.0)
+        want, lse, weights, tol, rel = attend64(p, q, dim ** -0.5, True, window)
+        for weigh in (False, True):
+            out, got_lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV)
+            w = torch.zeros(1, 2, n, device=DEV) if weigh else None
+            attend_raw(p, q, out, got_lse, window=window, w_out=w)
+            assert ((out.double() - want).abs() <= tol).all(), (n, weigh)
+            assert ((got_lse.double() - lse).abs() <= rel + 2.0 ** -21 * (1 + lse.abs())).all()
+            if weigh:
+                e = (w[0].double() - weights[0]).abs()
+                assert (e <= weights[0] * (rel + 2.0 ** -20 * (1 + 40)) + 2.0 ** -22 * weights[0]).all()
