@@ -60,7 +60,8 @@ __global__ void __launch_bounds__(kRowThreads, APPEND ? 8 : 6) k_rows(const Rows
         const int begin = q_begin(B, lo), end = q_begin(B, lo + 1);
         place[threadIdx.x][0] = place[threadIdx.x][1] = -1;
         if (t >= begin && t < end) {
-            const int n = kv_length(B, lo, true), slot = n - (end - begin) + (t - begin);
+            // (of a length that kv_length had to cut nothing is written: the slots at the bound hold older tokens)
+            const int n = kv_length(B, lo, true), slot = n == B.kv_len[lo] ? n - (end - begin) + (t - begin) : -1;
             const int page = slot < 0 ? -1 : B.table[lo * B.table_stride + B.page_of(slot)];
             if (slot < 0) atomicOr(B.status, kBadLength);
             else if (page < 0 || page >= B.num_pages) atomicOr(B.status, kBadPage);

@@ -716,3 +716,30 @@ def test_attend_workspace_of_any_content(fd, dtype, dim, new, group, mask):
             if weigh:
                 e = (w[0].double() - weights[0]).abs()
                 assert (e <= weights[0] * (rel + 2.0 ** -20 * (1 + 40)) + 2.0 ** -22 * weights[0]).all()
+
+
+@pytest.mark.parametrize("how", ["bound", "table", "negative"])
+def test_append_beyond_the_bounds_writes_nothing(fd, how):
+    """A sequence whose length is out of range is not written at all: cut to the bound, its new tokens would land on older ones."""
+    p = Pool(fd, 5, [300, 40], [4, 4], 2, 64, 16, BF16)
+    batch = p.batch
+    if how == "bound":
+        batch = fd.KVBatch(p.table, p.kv_len, p.q_start, 8, 4, 299)
+    if how == "table":
+        p.kv_len[0] = p.cols * 16 + 1
+        batch = fd.KVBatch(p.table, p.kv_len, p.q_start, 8, 4, 1000)
+    if how == "negative":
+        p.kv_len[0] = -1
+    before = p.k.clone(), p.v.clone()
+    k, v, q = (randn(s, 8, h, 64, dtype=BF16) for s, h in ((1, 2), (2, 2), (3, 4)))
+    pos = torch.arange(8, dtype=torch.int32, device=DEV)
+    freqs = fd.fd_rotary_frequencies(64, device=DEV)
+    qo = p.cache.append(batch, k, v, positions=pos, freqs=freqs, q=q)
+    with pytest.raises(fd.FdError) as e:
+        p.cache.synchronize()
+    assert e.value.status == fd.FD_ERR_INVALID
+    assert torch.equal(qo, fd.fd_rotary(q, pos, freqs))
+    pg, r = p.where(1, torch.arange(36, 40, device=DEV))
+    before[0][pg, r], before[1][pg, r] = fd.fd_rotary(k, pos, freqs)[4:], v[4:]
+    for got, want in zip((p.k, p.v), before):
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
