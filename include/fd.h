@@ -401,7 +401,7 @@ typedef struct {
 } fd_kv_desc;
 
 typedef struct {
-    const int32_t* table_dev; int64_t table_stride;           /* [batch][max_pages] */
+    const int32_t* table_dev; int64_t table_stride;           /* [batch][max_pages]; rows may overlap (stride 0: one for all) */
     const int32_t* kv_len_dev;                                /* [batch] */
     const int32_t* q_start_dev;                               /* [batch + 1] */
     int32_t batch, max_pages, total_q, max_new, max_len;

@@ -463,6 +463,15 @@ def _heads(t: torch.Tensor, dtype, index: int, head_dim: int, tokens: int, what:
     return t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d, h
 
 
+def _table(t: torch.Tensor, what: str):
+    """(stride, pages) of the rows of a page table; rows may lie in any distance, 0 (one row for all sequences, an expanded tensor) included."""
+    rows, cols = t.shape
+    row, unit = t.stride()
+    if unit != 1 and cols != 1:
+        _refuse(f"{what}: [batch, pages], unit stride inside a row")
+    return row if rows > 1 else cols, cols
+
+
 class _Messages(threading.local):
     def __init__(self):
         self.buf = ctypes.create_string_buffer(256)
@@ -534,14 +543,13 @@ class KVBatch:
         _need_tensor(kv_len, torch.int32, 1, dev.index, "kv_len")
         _need_tensor(q_start, torch.int32, 1, dev.index, "q_start")
         n = page_table.shape[0]
-        _need(page_table.stride(1) == 1 or page_table.shape[1] == 1, "page_table: unit stride inside a row")
+        stride, cols = _table(page_table, "page_table")
         _need(kv_len.shape[0] == n and q_start.shape[0] == n + 1 and kv_len.is_contiguous() and q_start.is_contiguous(),
               f"kv_len: {n} contiguous values, q_start: {n + 1}")
         self.device, self.total_q = dev, int(total_q)
         self.page_table, self.kv_len, self.q_start = page_table, kv_len, q_start
         self.batch, self.max_len = n, int(max_len)
-        self.struct = fd_kv_batch(page_table.data_ptr(), max(page_table.stride(0), page_table.shape[1]), kv_len.data_ptr(), q_start.data_ptr(), n,
-                                  page_table.shape[1], total_q, max_new, max_len)
+        self.struct = fd_kv_batch(page_table.data_ptr(), stride, kv_len.data_ptr(), q_start.data_ptr(), n, cols, total_q, max_new, max_len)
         self.ref = byref(self.struct)
 
 
@@ -666,10 +674,9 @@ class KVCache:
             _refuse("weights and weights_out: equal shapes")
         table = batch.page_table if new_table is None else new_table
         _need_tensor(table, torch.int32, 2, index, "new_table")
-        rows, cols = table.shape
-        row, unit = table.stride()
-        if rows != batch.batch or (unit != 1 and cols != 1):
-            _refuse("new_table: [batch, pages], unit stride inside a row")
+        stride, cols = _table(table, "new_table")
+        if table.shape[0] != batch.batch:
+            _refuse(f"new_table: {batch.batch} rows")
         if kept is None:
             kept = torch.empty((batch.batch, self.heads, max(keep, 0)), dtype=torch.int32, device=self.device)
         if new_len is None:
@@ -680,7 +687,7 @@ class KVCache:
             _refuse(f"kept: [{batch.batch}, {self.heads}, {keep}], contiguous")
         if new_len.numel() != batch.batch or not new_len.is_contiguous():
             _refuse(f"new_len: {batch.batch} contiguous values")
-        _call(index, lib.fd_kv_evict, self._h, ref, _EVICT.pack(weights.data_ptr(), weights_out.data_ptr(), w_stride, table.data_ptr(), max(row, cols), cols,
+        _call(index, lib.fd_kv_evict, self._h, ref, _EVICT.pack(weights.data_ptr(), weights_out.data_ptr(), w_stride, table.data_ptr(), stride, cols,
                                                                 keep, first, recent, kept.data_ptr(), new_len.data_ptr()))
         return kept, new_len, weights_out
 

@@ -82,7 +82,7 @@ fd_status check_batch(const Err& err, const fd_kv* kv, const fd_kv_batch* b, boo
     if (b->batch < 0 || b->batch > 65535) return err(FD_ERR_INVALID, "batch = %d: 0 to 65535", b->batch);
     if (b->batch == 0) return FD_OK;
     if (!b->table_dev || !b->kv_len_dev || (queries && !b->q_start_dev)) return err(FD_ERR_INVALID, "page table, lengths and starts must be non-null");
-    if (b->max_pages < 1 || b->table_stride < b->max_pages) return err(FD_ERR_INVALID, "bad page table: %d pages a row, stride %lld", b->max_pages, (long long)b->table_stride);
+    if (b->max_pages < 1 || b->table_stride < 0) return err(FD_ERR_INVALID, "bad page table: %d pages a row, stride %lld", b->max_pages, (long long)b->table_stride);
     if (b->total_q < 0 || b->max_new < 0 || b->max_new > b->total_q || (b->max_new == 0 && b->total_q > 0) || b->max_len < 0) return err(FD_ERR_INVALID, "bad bounds: total_q %d, max_new %d, max_len %d", b->total_q, b->max_new, b->max_len);
     if (b->max_len > (1 << 30) || b->total_q > (1 << 30)) return err(FD_ERR_UNSUPPORTED, "lengths up to 2^30 tokens are covered");
     return FD_OK;
@@ -368,6 +368,7 @@ fd_status fd_kv_evict(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_evict_a
     if (!x->weights_in_dev || !x->weights_out_dev || !x->kept_dev || !x->new_len_dev || !x->new_table_dev) return err(FD_ERR_INVALID, "weights, kept, new_len and new_table must be non-null");
     if (x->keep < 1 || x->first < 0 || x->recent < 0 || (int64_t)x->first + x->recent > x->keep) return err(FD_ERR_INVALID, "keep = %d, first = %d, recent = %d", x->keep, x->first, x->recent);
     if (x->weights_stride < b->max_len) return err(FD_ERR_INVALID, "weights: stride %lld is below max_len = %d", (long long)x->weights_stride, b->max_len);
+    // (written to: no two sequences may have a page in common, which rows that overlap would)
     if (x->new_max_pages < 1 || x->new_table_stride < x->new_max_pages) return err(FD_ERR_INVALID, "bad new page table: %d pages a row, stride %lld", x->new_max_pages, (long long)x->new_table_stride);
     if (x->new_max_pages < ceil_div(x->keep < b->max_len ? x->keep : b->max_len, d.page_size)) return err(FD_ERR_INVALID, "new page table: %d pages a row hold fewer tokens than are kept", x->new_max_pages);
     FD_TRY(check_device(err, kv));

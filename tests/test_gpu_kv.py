@@ -743,3 +743,24 @@ def test_append_beyond_the_bounds_writes_nothing(fd, how):
     before[0][pg, r], before[1][pg, r] = fd.fd_rotary(k, pos, freqs)[4:], v[4:]
     for got, want in zip((p.k, p.v), before):
         assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("new", [1, 2, 40])
+def test_page_table_of_one_row_for_all(fd, new):
+    """Sequences that continue one prompt read the same pages through an expanded table, up to lengths of their own."""
+    p = Pool(fd, 5, [700], [new], 2, 64, 16, BF16)
+    lengths = [700, 650, 300]
+    kv_len = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    start = torch.arange(4, dtype=torch.int32, device=DEV) * new
+    q = randn(6, 3 * new, 4, 64, dtype=BF16)
+    w, w_ref = torch.zeros(3, 2, 700, device=DEV), torch.zeros(3, 2, 700, device=DEV)
+    shared = fd.KVBatch(p.table.expand(3, -1), kv_len, start, 3 * new, new, 700)
+    copied = fd.KVBatch(p.table.repeat(3, 1), kv_len, start, 3 * new, new, 700)
+    out, lse = p.cache.attend(shared, q, weights=w)
+    ref, ref_lse = p.cache.attend(copied, q, weights=w_ref)
+    assert torch.equal(out, ref) and torch.equal(lse, ref_lse) and torch.equal(w, w_ref)
+    p.cache.synchronize()
+    launches = fd.fd_launch_count()
+    with pytest.raises(fd.FdError):                          # in place, or to pages in common
+        p.cache.evict(shared, w, 10)
+    assert fd.fd_launch_count() == launches

@@ -109,3 +109,19 @@ def test_packed_arguments(fd):
 
         want = [next(values) for _ in fields(st)]
         assert read(st.from_buffer_copy(fmt.pack(*want))) == want
+
+
+def test_page_table_strides(fd):
+    """Rows of a page table in any distance; an expanded one (every sequence reads the same pages) has stride 0, and its next row is not behind the first."""
+    import torch
+    from paper_2609_38198_b200 import binding as b
+    t = torch.arange(24, dtype=torch.int32).view(4, 6)
+    for x in (t, t[:, :3], t[::2], t[:1].expand(5, 6), t[:1, :2].expand(3, 2), t[:, 1:2], t.t()[:, :1], torch.as_strided(t, (4, 6), (2, 1)), t[:1], t[:, :0]):
+        stride, cols = b._table(x, "table")
+        assert cols == x.shape[1]
+        for r in range(x.shape[0]):
+            for c in range(cols):
+                assert x.storage_offset() + r * stride + c < t.numel() and int(x[r, c]) == x.storage_offset() + r * stride + c
+    for x in (t.t(), t[:, ::2]):
+        with pytest.raises(fd.FdError):
+            b._table(x, "table")
