@@ -4,11 +4,11 @@
 // head.  Per tile of 128 cached tokens:
 //   S = Q K^T         (Q in shared memory, K by TMA page by page) into 128 fp32 columns of TMEM;
 //   m, P = 2^(c S - c m)   one thread a row: the maximum over the tile, then exponentials, rounded to the element type and written back over S.
-//                     The maximum in use is raised only when a row exceeds it by 2^8: weights up to 2^8 lose nothing in floating point, and the
-//                     accumulator is read back and rescaled in the first tiles only;
+//                     The maximum in use is raised only when a row exceeds it by 2^8 (fp16: 2^5, see Elem): weights above 1 lose nothing in floating
+//                     point, and the accumulator is read back and rescaled in the first tiles only;
 //   O += P V          (P in TMEM, V row-major in shared memory as an MN-major operand) into D fp32 columns.
 // While one tile's rows are exponentiated the tensor core works on the other's.  Rounding P to 16 bits changes a weight by half an ulp at
-// most, independently per weight; the norm sums the unrounded weights in fp32.
+// most (fp16: or 2^-35 of the largest), independently per weight, which the operand of a tensor product costs; the norm sums the unrounded weights in fp32.
 //
 // Bounds: the tensor core (2 x 1024 clocks for two row tiles of 128 coordinates) and the MUFU (2 x 1024) could be busy all the time; what a pass takes is the chain
 // of one row tile -- scores ready, 600 clocks to read them and find the maximum, 1430 for 128 exponentials of one warp, 950 until the product and the next
@@ -58,6 +58,10 @@ __device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, v
         }
     return true;
 }
+// (see Elem; 2 x 2048 fp16 tokens with weights: 605 us with 2^8, 608 with 2^6, 618 with 2^5, 631 with 2^4)
+template <class T> constexpr float kLazy = 8.f;
+template <> constexpr float kLazy<__half> = 5.f;
+template <class T> constexpr float kShift = Elem<T>::kTop - kLazy<T>;
 // Instruction descriptor, fp32 accumulation, M = 128; `mn`: the B operand is MN-major.
 template <class T> constexpr uint32_t idesc_kv(int n, bool mn) {
     return (1u << 4) | (Elem<T>::kFormat << 7) | (Elem<T>::kFormat << 10) | ((mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
@@ -370,7 +374,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     mx[k] = max_nan(y[0], y[1]);
                 }
                 const float top = max_nan(max_nan(mx[0], mx[1], mx[2]), mx[3], m);
-                const bool raise = !((top - m) * c <= kLazy) && top != m;        // (first tile: from -inf; a NaN goes through)
+                const bool raise = !((top - m) * c <= kLazy<T>) && top != m;        // (first tile: from -inf; a NaN goes through)
                 if (__any_sync(~0u, raise)) {
                     const float alpha = raise ? ex2f((m - top) * c) : 1.0f;
                     if (raise) m = top;
@@ -390,7 +394,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         tmem_wait_st();
                     }
                 }
-                const float mc = m == -INFINITY ? 0.f : m * c;
+                const float mc = m == -INFINITY ? 0.f : m * c - kShift<T>;
                 const uint64_t cc = pair2(c, c), mm = pair2(-mc, -mc);
                 uint64_t sum[2] = {0, 0};
                 if (!kHold) tmem_ld32(s_addr, s[0]);
@@ -438,8 +442,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             const int64_t row = w.begin + token;
             const bool odd = num > 0 && *(volatile int*)&bars->odd;
             if (valid) {
-                if (a.splits > 1) a.part_lse[(split * (int64_t)a.batch.total_q + row) * a.q_heads + head] = empty ? -INFINITY : m * c + log2f(l);
-                else if (a.lse) a.lse[row * a.q_heads + head] = empty ? -INFINITY : (float)((double)(m * c + log2f(l)) * 0.69314718055994530942);
+                if (a.splits > 1) a.part_lse[(split * (int64_t)a.batch.total_q + row) * a.q_heads + head] = empty ? -INFINITY : (m * c - kShift<T>) + log2f(l);
+                else if (a.lse) a.lse[row * a.q_heads + head] = empty ? -INFINITY : (float)((double)((m * c - kShift<T>) + log2f(l)) * 0.69314718055994530942);
             }
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {

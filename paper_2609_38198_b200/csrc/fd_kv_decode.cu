@@ -19,6 +19,10 @@ namespace kv {
 namespace {
 
 constexpr int kWarpsFew = 4;
+// (see Elem; raising the maximum costs little beside the cache's bytes)
+template <class T> constexpr float kLazy = 8.f;
+template <> constexpr float kLazy<__half> = 3.f;
+template <class T> constexpr float kShift = Elem<T>::kTop - kLazy<T>;
 
 template <int D>
 struct GeoFew {
@@ -254,7 +258,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                 top[r] = m[r];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) top[r] = max_nan(top[r], s[n][2 * r], s[n][2 * r + 1]);
-                raise |= !((top[r] - m[r]) * c <= kLazy) && top[r] != m[r];
+                raise |= !((top[r] - m[r]) * c <= kLazy<T>) && top[r] != m[r];
             }
             if (__any_sync(~0u, raise)) {
 #pragma unroll
@@ -271,13 +275,15 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
             uint32_t p[NT / 2][4];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const float mc = m[r] == -INFINITY ? 0.f : m[r] * c;
+                const float mc = m[r] == -INFINITY ? 0.f : m[r] * c - kShift<T>;
+                float sum = 0.f;                     // (of the chunk first: beside one large weight every addition loses up to half a step of it)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float e0 = ex2f(fmaf(s[n][2 * r], c, -mc)), e1 = ex2f(fmaf(s[n][2 * r + 1], c, -mc));
-                    l[r] += e0 + e1;
+                    sum += e0 + e1;
                     p[n / 2][2 * (n % 2) + r] = Elem<T>::pack(e0, e1);
                 }
+                l[r] += sum;
             }
 #pragma unroll
             for (int x = 0; x < KEYS / 16; ++x) {
@@ -360,7 +366,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                     }
                 }
             }
-            const float lse2 = top == -INFINITY ? -INFINITY : top * c + log2f(sum);
+            const float lse2 = top == -INFINITY ? -INFINITY : (top * c - kShift<T>) + log2f(sum);
             if (cta0 != cta1) {
                 // (zeros, where the row sees nothing of the part: the join multiplies every part's result by a factor, which is 0 there)
                 if (d == 0) a.part_lse[slot * kFewRows + row] = lse2;

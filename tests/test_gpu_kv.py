@@ -764,3 +764,42 @@ def test_page_table_of_one_row_for_all(fd, new):
     with pytest.raises(fd.FdError):                          # in place, or to pages in common
         p.cache.evict(shared, w, 10)
     assert fd.fd_launch_count() == launches
+
+
+@pytest.mark.parametrize("new", [1, 64])
+@pytest.mark.parametrize("above", [10, 16, 17, 18])
+@pytest.mark.parametrize("spread", [0.0, 0.5])
+def test_attend_one_key_above_all(fd, new, above, spread):
+    """One key whose score lies far above 32767 others and whose value is 0, in as many caches as keep the GPU busy without cutting one: in fp16 a weight keeps
+    its 11 bits down to 2^-24 of the largest, and is off by 2^-35 of it below (fp16's normal range ends at 2^-14, its steps at 2^-24; the largest weight
+    is held at 2^10 or more; with few rows at 2^12 or more)."""
+    n, dim, heads, batch = 32768, 64, 8, 37
+    g = torch.Generator(device=DEV).manual_seed(above)
+    k = torch.zeros(n // 64, 64, heads, dim, dtype=FP16, device=DEV)
+    v = (1 + torch.rand(n // 64, 64, heads, dim, device=DEV, generator=g)).half()
+    if spread:
+        k[..., 1] = spread * torch.randn(n // 64, 64, heads, device=DEV, generator=g).half()
+    place = 70 if spread else n - 100
+    k[place // 64, place % 64] = 0
+    k[place // 64, place % 64, :, 0] = above
+    v[place // 64, place % 64] = 0
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    cache = fd.KVCache(k, v)
+    table = torch.arange(n // 64, dtype=torch.int32, device=DEV)[None].repeat(batch, 1)
+    q = torch.zeros(batch * new, heads, dim, dtype=FP16, device=DEV)
+    q[:, :, :2] = 8.0
+    out, lse = cache.attend(fd.KVBatch(table, i32([n] * batch), i32([new * b for b in range(batch + 1)]), batch * new, new, n), q, causal=False)
+    cache.synchronize()
+    for h in (0, heads - 1):
+        s = q[:1, h].double() @ k[:, :, h].reshape(n, dim).double().T / 8
+        p = torch.softmax(s, -1)
+        vv = v[:, :, h].reshape(n, dim).double()
+        want = p @ vv
+        # a rounded weight, the exponential, and 2^-12 for sums of one sign (see test_attend_long_sums_of_one_sign); the rounded result
+        tol = (2.0 ** -11 + 2.0 ** -12 + 2.0 ** -19) * want + 2.0 ** (-37 if new == 1 else -35) * p.max() * vv.sum(0) + torch.finfo(FP16).eps / 2 * want + 2.0 ** -25
+        err = (out[:, h].double() - want).abs()
+        assert (err <= tol).all(), float((err / want).max())
+        # the norm: 256 additions (of 32 tokens by each of four warps, or of 128) beside the one large weight, each off by half a step of it or less; the
+        # exponentials, the logarithm and the largest score
+        sure = 256 * 2.0 ** -24 + 2.0 ** -22 * (8 + above)
+        assert (lse[:, h].double() - torch.logsumexp(s, -1)).abs().max() <= sure
