@@ -359,7 +359,8 @@ fd_status fd_unit_peaks(void* scratch_dev, size_t scratch_bytes, void* cuda_stre
  *   All three arrays are read on the device, so a captured call takes its lengths at replay; total_q, max_new and max_len are
  *   upper bounds that size the launch.  A page number outside the pool, or a length outside [0, min(max_len,
  *   max_pages * page_size)], is never followed: the tokens of such a page count as zeros, the length is clamped; appends write neither
- *   to such a page nor any token of a sequence with such a length; and fd_kv_synchronize reports FD_ERR_INVALID.
+ *   to such a page nor any token of a sequence with such a length; and fd_kv_synchronize reports FD_ERR_INVALID.  max_new chooses attention's kernel: where
+ *   max_new times the query heads of a cached head is 16 or less, a sequence with more new tokens counts as having none and is reported likewise.
  * Positions: angles are taken in fp64 as position * freqs[i] and reduced there, so far positions lose nothing.
  * Masks: new token i of a sequence stands at slot p = kv_len - new + i.  Causal: it sees slots <= p; window > 0: of these
  *   the last `window`.  A row that sees nothing gets zeros and lse = -inf.  What a row does not see cannot reach it, not as an infinity or NaN either.

@@ -69,7 +69,7 @@ __device__ __forceinline__ Work few_work(const AttendArgs& a, int b, bool report
     Work w;
     w.b = b; w.begin = q_begin(a.batch, b); w.count = max(0, q_begin(a.batch, b + 1) - w.begin); w.t0 = 0;
     w.n = kv_length(a.batch, b, report);
-    if (w.count > kFewRows / a.group) {
+    if (w.count > a.few_rows / a.group) {
         if (report) atomicOr(a.batch.status, kBadLength);
         w.count = 0;
     }
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_few_join(const AttendArgs a, c
     const int block = blockIdx.x - weigh, r = block % a.few_rows, h = block / a.few_rows % a.heads;
     const int b = block / (a.few_rows * a.heads), begin = q_begin(a.batch, b), count = max(0, q_begin(a.batch, b + 1) - begin);
     const Parts parts = few_parts(a, b, h);                      // (anything, where nothing is new)
-    if (r >= count * a.group || count > kFewRows / a.group || parts.count == 1) return;        // one part: written by its CTA
+    if (r >= count * a.group || count > a.few_rows / a.group || parts.count == 1) return;        // one part: written by its CTA
     constexpr int E = D / 32;
     float o[E], top = -INFINITY, sum = 0.f;
 #pragma unroll

@@ -803,3 +803,20 @@ def test_attend_one_key_above_all(fd, new, above, spread):
         # exponentials, the logarithm and the largest score
         sure = 256 * 2.0 ** -24 + 2.0 ** -22 * (8 + above)
         assert (lse[:, h].double() - torch.logsumexp(s, -1)).abs().max() <= sure
+
+
+def test_attend_more_new_tokens_than_promised_few(fd):
+    """As above, with no more rows than the kernel for few rows holds: every row of the sequence is left out, whatever parts the caches are cut into."""
+    for n in (60, 5000):
+        p = Pool(fd, 5, [300, n], [1, 3], 2, 64, 16, BF16)
+        q = randn(6, 4, 4, 64, dtype=BF16)
+        good, _ = p.cache.attend(p.batch, q)
+        out = torch.full_like(q, 7.0)
+        w = torch.rand(2, 2, max(n, 300), device=DEV)
+        w0 = w.clone()
+        p.cache.attend(fd.KVBatch(p.table, p.kv_len, p.q_start, 4, 1, max(n, 300)), q, out=out, weights=w)
+        with pytest.raises(fd.FdError) as e:
+            p.cache.synchronize()
+        assert e.value.status == fd.FD_ERR_INVALID
+        assert ((out[0].double() - good[0].double()).abs() <= 2.0 ** -7 * good[0].double().abs() + 2.0 ** -9).all()
+        assert (out[1:] == 7.0).all() and torch.equal(w[1], w0[1])
