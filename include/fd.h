@@ -355,7 +355,8 @@ fd_status fd_unit_peaks(void* scratch_dev, size_t scratch_bytes, void* cuda_stre
  * Heads: a tensor of heads is [token][head][head_dim] with unit stride inside a head; the other strides are free.
  * Pages: token t of a sequence is row t % page_size of the pool's page table[t / page_size]; page_size is a multiple of 8.
  * Lengths: sequence i has kv_len[i] tokens in the cache, the q_start[i + 1] - q_start[i] new ones among them, at the end; the new
- *   tokens of all sequences follow each other in q, k, v and out.  Rows from q_start[batch] on (padding) are neither read into a result nor written.
+ *   tokens of all sequences follow each other in q, k, v and out.
+ *   Rows before q_start[0] (of sequences that another call takes) and from q_start[batch] on (padding) are neither read into a result nor written.
  *   All three arrays are read on the device, so a captured call takes its lengths at replay; total_q, max_new and max_len are
  *   upper bounds that size the launch.  A page number outside the pool, or a length outside [0, min(max_len,
  *   max_pages * page_size)], is never followed: the tokens of such a page count as zeros, the length is clamped; appends write neither

@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(256) k_join(const AttendArgs a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, me = W == 1 ? lane : (int)threadIdx.x;
     const int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + warp : blockIdx.x;
     const int64_t rows = (int64_t)q_begin(a.batch, a.batch.batch) * a.q_heads, all = (int64_t)a.batch.total_q * a.q_heads;
-    if (row >= rows) return;
+    if (row >= rows || row < (int64_t)q_begin(a.batch, 0) * a.q_heads) return;             // (of no sequence)
     float* f = W == 1 ? s_f + 32 * warp : s_f;
     float top = -INFINITY;
     for (int s = me; s < a.splits; s += 32 * W) top = max_nan(top, f[s] = a.part_lse[s * all + row]);

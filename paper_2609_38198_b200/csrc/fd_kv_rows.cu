@@ -39,8 +39,9 @@ __global__ void __launch_bounds__(kRowThreads, APPEND ? 8 : 6) k_rows(const Rows
     using V = Vec<T, VEC>;
     grid_wait();
     grid_go();
-    const int live = APPEND ? q_begin(a.batch, a.batch.batch) : a.tokens;       // (an append may be padded)
-    const int t0 = blockIdx.x * block_tokens, nt = max(0, min(block_tokens, live - t0));
+    // (an append may be padded, and its first tokens may belong to no sequence)
+    const int live = APPEND ? q_begin(a.batch, a.batch.batch) : a.tokens;
+    const int b0 = blockIdx.x * block_tokens, t0 = APPEND ? max(b0, q_begin(a.batch, 0)) : b0, nt = max(0, min(block_tokens - (t0 - b0), live - t0));
     const int half = a.rot / 2;
     for (int i = threadIdx.x; i < nt * half; i += kRowThreads) {
         const int t = i / half, f = i - t * half;

@@ -820,3 +820,26 @@ def test_attend_more_new_tokens_than_promised_few(fd):
         assert e.value.status == fd.FD_ERR_INVALID
         assert ((out[0].double() - good[0].double()).abs() <= 2.0 ** -7 * good[0].double().abs() + 2.0 ** -9).all()
         assert (out[1:] == 7.0).all() and torch.equal(w[1], w0[1])
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_rows_before_the_first_sequence(fd, new):
+    """A batch may be the tail of a larger one (decoding sequences behind prompts in the same tensors): rows before its first are left as they were."""
+    p = Pool(fd, 5, [5000], [new], 1, 64, 16, BF16)
+    p.q_start += 4
+    batch = fd.KVBatch(p.table, p.kv_len, p.q_start, new + 4, new, 5000)
+    q = randn(6, new + 4, 4, 64, dtype=BF16)
+    k, v = randn(1, new + 4, 1, 64, dtype=BF16), randn(2, new + 4, 1, 64, dtype=BF16)
+    pos = torch.arange(new + 4, dtype=torch.int32, device=DEV)
+    freqs = fd.fd_rotary_frequencies(64, device=DEV)
+    turned = fd.fd_rotary(q, pos, freqs)
+    qo = q.clone()
+    p.cache.append(batch, k, v, positions=pos, freqs=freqs, q=qo, q_out=qo)
+    p.cache.synchronize()
+    assert torch.equal(qo[4:], turned[4:]) and torch.equal(qo[:4], q[:4])
+    out, lse = torch.full_like(q, 7.0), torch.full((new + 4, 4), 7.0, device=DEV)
+    p.batch = batch
+    attend_raw(p, qo, out, lse)
+    assert (out[:4] == 7.0).all() and (lse[:4] == 7.0).all()
+    ref, ref_lse = p.cache.attend(fd.KVBatch(p.table, p.kv_len, p.q_start - 4, new, new, 5000), qo[4:])
+    assert ((out[4:].double() - ref.double()).abs() <= 2.0 ** -7 * ref.double().abs() + 2.0 ** -9).all() and (lse[4:] - ref_lse).abs().max() < 1e-5
