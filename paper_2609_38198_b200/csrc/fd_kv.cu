@@ -127,7 +127,7 @@ Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weight
         p.part_lse = (size_t)2 * p.ctas * kFewRows;
         if (weights) {
             p.score_stride = round_up(b->max_len, 64);
-            p.scores = (size_t)b->batch * heads * kFewRows * p.score_stride;
+            p.scores = (size_t)b->batch * heads * b->max_new * group * p.score_stride;
         }
         return p;
     }
@@ -330,7 +330,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
         if (need && (!workspace_dev || workspace_bytes < need)) return err(FD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
         if (need && (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return err(FD_ERR_INVALID, "workspace must be 16-byte aligned");
         few = p.few;
-        a.row_tiles = p.row_tiles; a.splits = p.splits; a.split_tiles = p.split_tiles; a.ctas = p.ctas; a.few_rows = b->max_new * a.group;
+        a.row_tiles = p.row_tiles; a.splits = p.splits; a.split_tiles = p.split_tiles; a.ctas = p.ctas; a.few_rows = few ? b->max_new * a.group : 0;
         a.parts = static_cast<int2*>(workspace_dev);
         a.part_o = static_cast<float*>(workspace_dev) + p.parts;
         a.part_lse = a.part_o + p.part_o;

@@ -104,7 +104,7 @@ struct AttendArgs {
     int ctas, few_rows;              // few rows: CTAs that share the batch's caches; rows a sequence has at most; first CTA and number of the parts of each
     int2* parts;                     // (sequence, head)
     float* part_o; float* part_lse;  // [split][token][query head]([head_dim]); few rows: [slot][kFewRows]([head_dim])
-    float* scores; int64_t score_stride;     // few rows and weights: scale_log2 q.k of every row and slot, [sequence][head][kFewRows][score_stride]
+    float* scores; int64_t score_stride;     // few rows and weights: scale_log2 q.k of every row and slot, [sequence][head][few_rows][score_stride]
     int box_rows;
     const void* v_pool; int64_t v_page, v_token, v_head;
 };

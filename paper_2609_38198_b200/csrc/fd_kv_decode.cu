@@ -205,7 +205,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
         float* score_row[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-            score_row[r] = a.scores && a.w_out && g + 8 * r < rows ? a.scores + (((int64_t)b * a.heads + h) * kFewRows + g + 8 * r) * a.score_stride + 2 * t : nullptr;
+            score_row[r] = a.scores && a.w_out && g + 8 * r < rows ? a.scores + (((int64_t)b * a.heads + h) * a.few_rows + g + 8 * r) * a.score_stride + 2 * t : nullptr;
 
         float o[D / 8][4];
 #pragma unroll
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_few_join(const AttendArgs a, c
         for (int64_t key0 = first; key0 < w.n; key0 += (int64_t)per * kWeighTokens) {
             float sum[4];
             const int key1 = (int)key0 + threadIdx.x;
-            const float* s = a.scores + ((int64_t)w.b * a.heads + h) * kFewRows * a.score_stride + key1;
+            const float* s = a.scores + ((int64_t)w.b * a.heads + h) * a.few_rows * a.score_stride + key1;
 #pragma unroll
             for (int k = 0; k < 4; ++k) sum[k] = 0.f;
             for (int r = 0; r < rows; ++r) {

@@ -843,3 +843,21 @@ def test_rows_before_the_first_sequence(fd, new):
     assert (out[:4] == 7.0).all() and (lse[:4] == 7.0).all()
     ref, ref_lse = p.cache.attend(fd.KVBatch(p.table, p.kv_len, p.q_start - 4, new, new, 5000), qo[4:])
     assert ((out[4:].double() - ref.double()).abs() <= 2.0 ** -7 * ref.double().abs() + 2.0 ** -9).all() and (lse[4:] - ref_lse).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("new,group", [(1, 1), (1, 4), (2, 3), (5, 3), (16, 1)])
+def test_attend_workspace_holds_the_rows_there_are(fd, new, group):
+    """Scores of few rows take 4 bytes a row and token of the bound, for the rows that max_new allows."""
+    import ctypes
+    p = Pool(fd, 5, [300, 1700], [new, min(new, 2)], 2, 64, 16, FP16)
+    q = randn(6, p.total, 2 * group, 64, dtype=FP16)
+    ref = ctypes.byref(p.batch.struct)
+    with_w, without = (fd.lib.fd_kv_attend_bytes(p.cache._h, ref, 2 * group, w) for w in (1, 0))
+    assert with_w - without == 4 * 2 * 2 * new * group * 1728            # (1700 rounded up to a multiple of 64)
+    want, _, weights, tol, rel = attend64(p, q, 0.125)
+    out, lse, w = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV), torch.zeros(2, 2, 1700, device=DEV)
+    attend_raw(p, q, out, lse, w_out=w)
+    assert ((out.double() - want).abs() <= tol).all()
+    for b, n in enumerate(p.kv):
+        e = (w[b, :, :n].double() - weights[b]).abs()
+        assert (e <= weights[b] * (rel + 2.0 ** -20 * (1 + 40)) + 2.0 ** -22 * weights[b]).all()
