@@ -20,7 +20,7 @@
 // Warps 0-3 / 4-7: softmax of row tile 0 / 1; 8: TMA; 9: MMA; 10, 11: values of tiles that some row sees only in part.  What a row does not see gets P = 0
 // exactly, but 0 x inf = NaN: in those tiles rows behind the sequence are zeroed in shared memory, and so are elements that are not finite; the latter
 // are added again at the end, row by row, to the rows that see them (never on finite data).
-// Every wait is bounded; on expiry the CTA raises a status word, lets its copies land, frees TMEM and exits.
+// Every wait is bounded; on expiry the CTA raises a status word, lets its copies and products end, frees TMEM and exits.
 #include <algorithm>
 
 #include "fd_kv_dev.h"
@@ -58,6 +58,11 @@ __device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, v
         }
     return true;
 }
+// Waits, bounded, for what a CTA that gives up has in flight.
+__device__ __forceinline__ void land(uint64_t* bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity) && clock64() - t0 < 20000000ll) {}
+}
 // (see Elem; 2 x 2048 fp16 tokens with weights: 605 us with 2^8, 608 with 2^6, 618 with 2^5, 631 with 2^4)
 template <class T> constexpr float kLazy = 8.f;
 template <> constexpr float kLazy<__half> = 5.f;
@@ -87,7 +92,7 @@ struct GeoAt {
 template <int SLOTS>
 struct Bars {
     uint64_t q_full, full[SLOTS], empty[SLOTS], clean[SLOTS];
-    uint64_t s_full[2], p_full[2][4], pv_done[2];
+    uint64_t s_full[2], p_full[2][4], pv_done[2], drained;
     uint32_t tmem_base;
     int abort_flag, odd;                                        // odd: elements that are not finite were taken out of a tile
 };
@@ -179,7 +184,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
 
     const int warp = warp_index(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        mbar_init(&bars->q_full, 1);
+        mbar_init(&bars->q_full, 1); mbar_init(&bars->drained, 1);
         for (int s = 0; s < A::kSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); mbar_init(&bars->clean[s], 2); }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&bars->s_full[t], 1); mbar_init(&bars->pv_done[t], 1);
@@ -197,6 +202,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
 
+    int issued = 0;                                                      // tiles of the ring that this warp has asked for
     if (warp >= kSoftWarps) {
         if (warp == kSoftWarps && num > 0) {
             // ---------------------------------------------------------------- TMA
@@ -217,14 +223,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 if (!ok) break;
                 load_tile<D>(ring + s * G::kTile, (it & 1) ? &map_v : &map_k, a, w, j0 + it / 2, h, &bars->full[s]);
             }
-            if (!ok && lane == 0) {             // aborted: copies in flight land before the CTA exits (bounded)
-                for (int k = max(0, it - A::kSlots); k < it; ++k) {
-                    const long long c0 = clock64();
-                    while (!mbar_try_wait(&bars->full[k % A::kSlots], (k / A::kSlots) & 1) && clock64() - c0 < 20000000ll) {}
-                }
-                const long long c0 = clock64();
-                while (!mbar_try_wait(&bars->q_full, 0) && clock64() - c0 < 20000000ll) {}
-            }
+            issued = it;
         } else if (warp == kSoftWarps + 1 && num > 0) {
             // ---------------------------------------------------------------- MMA (one thread)
             if (elect_one()) {
@@ -485,6 +484,14 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) {                                                   // whoever gave up: copies and products in flight end before the CTA does
+        if (warp == kSoftWarps && num > 0 && lane == 0) {
+            for (int k = max(0, issued - A::kSlots); k < issued; ++k) land(&bars->full[k % A::kSlots], (k / A::kSlots) & 1);
+            land(&bars->q_full, 0);
+        }
+        if (warp == kSoftWarps + 1 && elect_one()) { tc_commit(&bars->drained); land(&bars->drained, 0); }
+        __syncthreads();
+    }
     if (warp == kSoftWarps) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(A::kCols) : "memory");
     }
@@ -572,7 +579,7 @@ struct GeoWeigh {
 };
 template <int D>
 struct WeighBars {
-    uint64_t k_full, full[GeoWeigh<D>::kSlots], empty[GeoWeigh<D>::kSlots], s_full[2], s_empty[2], l_full[4];
+    uint64_t k_full, full[GeoWeigh<D>::kSlots], empty[GeoWeigh<D>::kSlots], s_full[2], s_empty[2], l_full[4], drained;
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -609,7 +616,7 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     const int key = key0 + (warp & 3) * 32 + lane;                            // of the first 8 warps
     float acc = 0.f;
     if (threadIdx.x == 0) {
-        mbar_init(&bars->k_full, 1);
+        mbar_init(&bars->k_full, 1); mbar_init(&bars->drained, 1);
         for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&bars->s_full[i], 1); mbar_init(&bars->s_empty[i], kWeighWarps); }
         for (int i = 0; i < 4; ++i) mbar_init(&bars->l_full[i], 1);
@@ -625,6 +632,7 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
 
+    int issued = 0;                                                           // row tiles that this thread has asked for
     if (warp == kWeighWarps && num > 0) {
         // -------------------------------------------------------------------- TMA
         load_tile<D>(k_base, &map_k, a, w, blockIdx.x, h, &bars->k_full);
@@ -639,14 +647,7 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
                 for (int c = 0; c < G::kChunks; ++c)
                     tma_load_3d(ring + s * G::kTile + c * G::kChunkBytes, &map_q, c * 64, h * a.group, w.begin + (q0 + it) * a.tile_tokens, &bars->full[s]);
             }
-            if (!ok) {
-                for (int k = max(0, it - kSlots); k < it; ++k) {
-                    const long long c0 = clock64();
-                    while (!mbar_try_wait(&bars->full[k % kSlots], (k / kSlots) & 1) && clock64() - c0 < 20000000ll) {}
-                }
-                const long long c0 = clock64();
-                while (!mbar_try_wait(&bars->k_full, 0) && clock64() - c0 < 20000000ll) {}
-            }
+            issued = it;
         }
     } else if (warp == kWeighWarps + 1 && num > 0) {
         // -------------------------------------------------------------------- MMA (one thread)
@@ -765,6 +766,14 @@ k_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUten
     if (warp < 4 && key < w.n && !*abort_flag) {
         const int64_t at = ((int64_t)b * a.heads + h) * a.w_stride + key;
         a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + (acc + s_acc[key - key0]);
+    }
+    if (*abort_flag) {                                                        // as in k_attend
+        if (warp == kWeighWarps && num > 0 && lane == 0) {
+            for (int k = max(0, issued - kSlots); k < issued; ++k) land(&bars->full[k % kSlots], (k / kSlots) & 1);
+            land(&bars->k_full, 0);
+        }
+        if (warp == kWeighWarps + 1 && elect_one()) { tc_commit(&bars->drained); land(&bars->drained, 0); }
+        __syncthreads();
     }
     if (warp == kWeighWarps) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kWeighCols) : "memory");
