@@ -460,6 +460,8 @@ def _heads(t: torch.Tensor, dtype, index: int, head_dim: int, tokens: int, what:
     st, sh, sd = t.stride()
     if n != tokens or d != head_dim or (sd != 1 and d != 1):
         _refuse(f"{what}: [{tokens}, heads, {head_dim}] with unit stride inside a head")
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(f"{what} requires a gradient, and no graph is built here: call under torch.no_grad() (the gradient of fd_rotary is fd_rotary with inverse=True)")
     return t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d, h
 
 
@@ -517,7 +519,7 @@ def _rotary_args(positions, freqs, tokens: int, index: int, layout: str):
 def fd_rotary(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, layout: str = "half", scale: float = 1.0,
               inverse: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotary positions of x [tokens, heads, head_dim] on the current stream; with `inverse` the transpose, which takes the gradient of the
-    result to the gradient of x.  `out` may be x."""
+    result to the gradient of x.  `out` may be x.  No graph is built: a tensor that requires a gradient is refused outside torch.no_grad()."""
     dt = x.dtype if isinstance(x, torch.Tensor) else None
     code = _DTYPES.get(dt)
     if code is None or not x.is_cuda or x.dim() != 3:
@@ -556,7 +558,8 @@ class KVBatch:
 class KVCache:
     """Keys and values in pages: two pools [page, token in page, head, head_dim] (any strides with unit stride inside a head, so a pool laid
     out [page, head, token, head_dim] is passed transposed).  Calls run on the current stream and mirror the C entry points; workspaces are
-    taken from the current stream's allocator for each call, so calls on several streams and captured graphs share nothing but the pools."""
+    taken from the current stream's allocator for each call, so calls on several streams and captured graphs share nothing but the pools.  No graph is
+    built: tensors that require a gradient are refused outside torch.no_grad()."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         _need(isinstance(k_pages, torch.Tensor) and k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in (torch.bfloat16, torch.float16),
@@ -564,6 +567,7 @@ class KVCache:
         dev = k_pages.device
         _need_tensor(v_pages, k_pages.dtype, 4, dev.index, "v_pages")
         _need(k_pages.shape == v_pages.shape and k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "k_pages, v_pages: equal shapes, unit stride inside a head")
+        _need(not ((k_pages.requires_grad or v_pages.requires_grad) and torch.is_grad_enabled()), "k_pages, v_pages require a gradient, and no graph is built here")
         self.device, self.dtype = dev, k_pages.dtype
         self.k_pages, self.v_pages = k_pages, v_pages
         pages, size, heads, d = k_pages.shape
@@ -657,6 +661,8 @@ class KVCache:
 
     def _check_weights(self, t: torch.Tensor, batch: KVBatch) -> int:
         _need_tensor(t, torch.float32, 3, self.device.index, "weights")
+        if t.requires_grad and torch.is_grad_enabled():
+            _refuse("weights require a gradient, and no graph is built here")
         n, h, length = t.shape
         if n != batch.batch or h != self.heads or length < batch.max_len or not t.is_contiguous():
             _refuse(f"weights: [{batch.batch}, {self.heads}, {batch.max_len} or more], contiguous")

@@ -861,3 +861,22 @@ def test_attend_workspace_holds_the_rows_there_are(fd, new, group):
     for b, n in enumerate(p.kv):
         e = (w[b, :, :n].double() - weights[b]).abs()
         assert (e <= weights[b] * (rel + 2.0 ** -20 * (1 + 40)) + 2.0 ** -22 * weights[b]).all()
+
+
+def test_tensors_that_need_a_gradient_are_refused(fd):
+    """The operators build no graph, so a gradient would be lost in silence."""
+    p = Pool(fd, 5, [30], [2], 2, 64, 16, BF16)
+    q, k, v = (randn(s, 2, h, 64, dtype=BF16).requires_grad_() for s, h in ((1, 4), (2, 2), (3, 2)))
+    w = torch.zeros(1, 2, 30, device=DEV).requires_grad_()
+    pos = torch.arange(2, dtype=torch.int32, device=DEV)
+    freqs = fd.fd_rotary_frequencies(64, device=DEV)
+    for call in (lambda: fd.fd_rotary(q, pos, freqs), lambda: p.cache.attend(p.batch, q), lambda: fd.KVCache(p.k.clone().requires_grad_(), p.v),
+                 lambda: p.cache.evict(p.batch, w, 10), lambda: p.cache.append(p.batch, k, v.detach()),
+                 lambda: p.cache.append(p.batch, k.detach(), v), lambda: p.cache.append(p.batch, k.detach(), v.detach(), positions=pos, freqs=freqs, q=q)):
+        launches = fd.fd_launch_count()
+        with pytest.raises(fd.FdError):
+            call()
+        assert fd.fd_launch_count() == launches
+        with torch.no_grad():
+            call()
+    p.cache.synchronize()
