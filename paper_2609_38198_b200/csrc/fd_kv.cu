@@ -108,6 +108,19 @@ bool overlap(const fd_heads& a, const fd_heads& b, int tokens, int head_dim, int
     range(a, &al, &ah); range(b, &bl, &bh);
     return al < bh && bl < ah;
 }
+// Whether no two rows of a result overlap: rows that lie dt tokens and dh heads apart begin dt * token_stride + dh * head_stride apart, which has to be head_dim or
+// more in either direction.
+bool rows_apart(const fd_heads& h, int tokens, int head_dim) {
+    const int64_t ts = h.token_stride, hs = h.head_stride;
+    if (tokens <= 1) return true;                                // (a head stride below head_dim is refused for every tensor)
+    if (ts < head_dim) return false;
+    if (ts >= (h.heads - 1) * hs + head_dim || h.heads == 1) return true;
+    for (int64_t dh = 1; dh < h.heads; ++dh) {                   // the two multiples of ts next to dh * hs
+        const int64_t dt = dh * hs / ts, rest = dh * hs % ts;
+        if ((rest < head_dim && dt < tokens) || (ts - rest < head_dim && dt + 1 < tokens)) return false;
+    }
+    return true;
+}
 bool same(const fd_heads& a, const fd_heads& b) { return a.p_dev == b.p_dev && a.token_stride == b.token_stride && a.head_stride == b.head_stride && a.heads == b.heads; }
 
 }  // namespace
@@ -182,8 +195,8 @@ fd_status fd_rotary(const fd_heads* x, const fd_heads* out, int32_t dtype, int32
     FD_TRY(check_rows(err, *x, head_dim, size, "x"));
     FD_TRY(check_rows(err, *out, head_dim, size, "out"));
     if (x->heads != out->heads || x->heads > 65536) return err(FD_ERR_INVALID, "x has %d heads, out %d", x->heads, out->heads);
+    if (!rows_apart(*out, tokens, head_dim)) return err(FD_ERR_INVALID, "out: rows overlap");
     if (!same(*x, *out) && overlap(*x, *out, tokens, head_dim, size)) return err(FD_ERR_INVALID, "out overlaps x without being x");
-    if (tokens > 1 && out->token_stride < head_dim) return err(FD_ERR_INVALID, "out: rows of two tokens overlap");
     int dev = 0, sms = 148;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -265,7 +278,7 @@ fd_status fd_kv_append(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_append
         FD_TRY(check_rows(err, x->q_out, d.head_dim, 2, "q_out"));
         if (x->q.heads != x->q_out.heads || x->q.heads > 65536) return err(FD_ERR_INVALID, "q has %d heads, q_out %d", x->q.heads, x->q_out.heads);
         if (!same(x->q, x->q_out) && overlap(x->q, x->q_out, b->total_q, d.head_dim, 2)) return err(FD_ERR_INVALID, "q_out overlaps q without being q");
-        if (b->total_q > 1 && x->q_out.token_stride < d.head_dim) return err(FD_ERR_INVALID, "q_out: rows of two tokens overlap");
+        if (!rows_apart(x->q_out, b->total_q, d.head_dim)) return err(FD_ERR_INVALID, "q_out: rows overlap");
     }
     FD_TRY(check_device(err, kv));
     RowsArgs a{};
@@ -304,7 +317,8 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
         if (x->q.heads != x->out.heads || x->q.heads % d.heads) return err(FD_ERR_INVALID, "q has %d heads, out %d, the cache %d", x->q.heads, x->out.heads, d.heads);
         if (x->q.heads / d.heads > 128) return err(FD_ERR_UNSUPPORTED, "%d query heads a cached head: up to 128 are covered", x->q.heads / d.heads);
         if (overlap(x->q, x->out, b->total_q, d.head_dim, 2)) return err(FD_ERR_INVALID, "out overlaps q");
-        if (b->total_q > 1 && (x->out.token_stride < d.head_dim || x->q.token_stride < d.head_dim)) return err(FD_ERR_INVALID, "rows of two tokens overlap");
+        if (b->total_q > 1 && x->q.token_stride < d.head_dim) return err(FD_ERR_INVALID, "q: rows of two tokens overlap");
+        if (!rows_apart(x->out, b->total_q, d.head_dim)) return err(FD_ERR_INVALID, "out: rows overlap");
     }
     if (!(x->scale > 0) || !(x->scale < 1e30)) return err(FD_ERR_INVALID, "scale must be positive");
     if (x->window < 0 || (x->window > 0 && !x->causal)) return err(FD_ERR_INVALID, "a window is positive and causal (0: none)");

@@ -880,3 +880,26 @@ def test_tensors_that_need_a_gradient_are_refused(fd):
         with torch.no_grad():
             call()
     p.cache.synchronize()
+
+
+def test_overlapping_rows_are_refused(fd):
+    """Results whose rows overlap each other, which would depend on the order of writing."""
+    p = Pool(fd, 5, [30, 20], [2, 1], 2, 64, 16, BF16)
+    q, k = randn(1, 3, 4, 64, dtype=BF16), randn(2, 3, 2, 64, dtype=BF16)
+    pos = torch.arange(3, dtype=torch.int32, device=DEV)
+    freqs = fd.fd_rotary_frequencies(64, device=DEV)
+    flat = torch.zeros(4096, dtype=BF16, device=DEV)
+    for strides in ((64, 64), (192, 64), (64, 128), (72, 64), (128, 64)):
+        bad = torch.as_strided(flat, (3, 4, 64), (*strides, 1))
+        with pytest.raises(fd.FdError):
+            fd.fd_rotary(q, pos, freqs, out=bad)
+        with pytest.raises(fd.FdError):
+            p.cache.append(p.batch, k, k, positions=pos, freqs=freqs, q=q, q_out=bad)
+        with pytest.raises(fd.FdError):
+            p.cache.attend(p.batch, q, out=bad)
+    assert (flat == 0).all()
+    ref, _ = p.cache.attend(p.batch, q)
+    for strides in ((256, 64), (64, 192), (264, 64), (72, 216)):         # token by token, head by head, with gaps
+        good = torch.as_strided(flat, (3, 4, 64), (*strides, 1))
+        assert torch.equal(p.cache.attend(p.batch, q, out=good)[0], ref)
+    p.cache.synchronize()

@@ -125,3 +125,20 @@ def test_page_table_strides(fd):
     for x in (t.t(), t[:, ::2]):
         with pytest.raises(fd.FdError):
             b._table(x, "table")
+
+
+@pytest.mark.parametrize("tokens,heads", [(1, 3), (2, 1), (2, 2), (3, 4), (7, 3)])
+def test_results_whose_rows_overlap_are_refused(fd, tokens, heads):
+    """Against every pair of rows.  Every call is refused before anything is launched: x lies over the first row of the result."""
+    from paper_2609_38198_b200 import binding
+    dim = 8
+    x = binding.fd_heads((1 << 16) + 4, heads * dim, dim, heads)
+    for ts in (8, 9, 16, 20, 24, 28, 32, 40, 64):
+        for hs in (8, 10, 12, 16, 20, 24, 56, 60):
+            at = sorted(t * ts + h * hs for t in range(tokens) for h in range(heads))
+            apart = all(b - a >= dim for a, b in zip(at, at[1:]))
+            err = ctypes.create_string_buffer(256)
+            st = fd.lib.fd_rotary(ctypes.byref(x), ctypes.byref(binding.fd_heads(1 << 16, ts, hs, heads)), fd.FD_FP32, tokens, dim, 256, 512, 8, 0, 1.0, 0,
+                                  None, err, 256)
+            assert st == fd.FD_ERR_INVALID and err.value == (b"out overlaps x without being x" if apart else b"out: rows overlap"), (ts, hs)
+    assert fd.fd_launch_count() == 0
