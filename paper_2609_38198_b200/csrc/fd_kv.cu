@@ -121,6 +121,12 @@ bool rows_apart(const fd_heads& h, int tokens, int head_dim) {
     }
     return true;
 }
+// Whether two arrays of `rows` rows of `len` elements of 4 bytes, `stride` elements apart in both, overlap without being the same.
+bool partly_over(const void* a, const void* b, int64_t rows, int64_t stride, int64_t len) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), d = x < y ? y - x : x - y, l = 4 * (uintptr_t)len, s = 4 * (uintptr_t)stride;
+    if (d == 0 || len <= 0 || d >= (uintptr_t)(rows - 1) * s + l) return false;
+    return d % s < l || s - d % s < l;                           // (rows of the one may lie between those of the other)
+}
 bool same(const fd_heads& a, const fd_heads& b) { return a.p_dev == b.p_dev && a.token_stride == b.token_stride && a.head_stride == b.head_stride && a.heads == b.heads; }
 
 }  // namespace
@@ -310,6 +316,8 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
     if (x->weights_out_dev) {
         if (!x->lse_dev && b->total_q > 0) return err(FD_ERR_INVALID, "weights need lse");
         if (x->weights_stride < b->max_len) return err(FD_ERR_INVALID, "weights: stride %lld is below max_len = %d", (long long)x->weights_stride, b->max_len);
+        if (x->weights_in_dev && partly_over(x->weights_in_dev, x->weights_out_dev, (int64_t)b->batch * d.heads, x->weights_stride, b->max_len))
+            return err(FD_ERR_INVALID, "weights_out overlaps weights_in without being it");
     } else if (x->weights_in_dev) return err(FD_ERR_INVALID, "weights_in without weights_out");
     if (b->total_q > 0) {
         FD_TRY(check_wide(err, x->q, d.head_dim, "q"));
@@ -382,6 +390,9 @@ fd_status fd_kv_evict(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_evict_a
     if (!x->weights_in_dev || !x->weights_out_dev || !x->kept_dev || !x->new_len_dev || !x->new_table_dev) return err(FD_ERR_INVALID, "weights, kept, new_len and new_table must be non-null");
     if (x->keep < 1 || x->first < 0 || x->recent < 0 || (int64_t)x->first + x->recent > x->keep) return err(FD_ERR_INVALID, "keep = %d, first = %d, recent = %d", x->keep, x->first, x->recent);
     if (x->weights_stride < b->max_len) return err(FD_ERR_INVALID, "weights: stride %lld is below max_len = %d", (long long)x->weights_stride, b->max_len);
+    if (partly_over(x->weights_in_dev, x->weights_out_dev, (int64_t)b->batch * d.heads, x->weights_stride, b->max_len))
+        return err(FD_ERR_INVALID, "weights_out overlaps weights_in without being it");
+    if (partly_over(x->new_len_dev, b->kv_len_dev, 1, b->batch, b->batch)) return err(FD_ERR_INVALID, "new_len overlaps kv_len without being it");
     // (written to: no two sequences may have a page in common, which rows that overlap would)
     if (x->new_max_pages < 1 || x->new_table_stride < x->new_max_pages) return err(FD_ERR_INVALID, "bad new page table: %d pages a row, stride %lld", x->new_max_pages, (long long)x->new_table_stride);
     if (x->new_max_pages < ceil_div(x->keep < b->max_len ? x->keep : b->max_len, d.page_size)) return err(FD_ERR_INVALID, "new page table: %d pages a row hold fewer tokens than are kept", x->new_max_pages);

@@ -398,7 +398,7 @@ cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream) {
     ++g_launches;
     e = launch_behind(stream, dim3(a.heads, a.batch.batch), dim3(many ? 1024 : 512), smem, many ? k_select<1024> : k_select<512>, a);
     if (e != cudaSuccess) return e;
-    const bool over = a.new_len < a.batch.kv_len + a.batch.batch && a.batch.kv_len < a.new_len + a.batch.batch;
+    const bool over = a.new_len == a.batch.kv_len;
     // blocks for about 16 KB in flight on every SM twice over, of 64 rows or more; in place as many as a row has slices of 64 bytes do work
     int shares = a.head_dim / 32;
     while (shares < 32 && 2 * (int64_t)shares * a.heads * a.batch.batch < 1200 && a.keep / (2 * shares) >= 64) shares *= 2;

@@ -903,3 +903,24 @@ def test_overlapping_rows_are_refused(fd):
         good = torch.as_strided(flat, (3, 4, 64), (*strides, 1))
         assert torch.equal(p.cache.attend(p.batch, q, out=good)[0], ref)
     p.cache.synchronize()
+
+
+def test_totals_and_lengths_that_overlap_are_refused(fd):
+    """weights_out may be weights and new_len may be kv_len; the one may not lie partly over the other."""
+    p = Pool(fd, 5, [30, 20], [2, 1], 2, 64, 16, BF16)
+    q = randn(1, 3, 4, 64, dtype=BF16)
+    totals = torch.zeros(400, device=DEV)
+    a, b = totals[:120].view(2, 2, 30), totals[8:128].view(2, 2, 30)
+    lengths = torch.tensor([30, 20, 0], dtype=torch.int32, device=DEV)
+    for x, y in ((a, b), (b, a)):
+        with pytest.raises(fd.FdError):
+            p.cache.attend(p.batch, q, weights=x, weights_out=y)
+        with pytest.raises(fd.FdError):
+            p.cache.evict(p.batch, x, 10, weights_out=y)
+    with pytest.raises(fd.FdError):
+        p.cache.evict(fd.KVBatch(p.table, lengths[:2], p.q_start, 3, 2, 30), a, 10, new_len=lengths[1:])
+    assert (totals == 0).all() and lengths.tolist() == [30, 20, 0]
+    p.cache.attend(p.batch, q, weights=a, weights_out=totals[120:240].view(2, 2, 30))
+    p.cache.attend(p.batch, q, weights=a, weights_out=a)
+    assert torch.equal(totals[:120], totals[120:240]) and float(totals.sum()) > 0
+    p.cache.synchronize()
