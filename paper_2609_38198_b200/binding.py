@@ -546,6 +546,7 @@ class KVBatch:
         _need_tensor(q_start, torch.int32, 1, dev.index, "q_start")
         n = page_table.shape[0]
         stride, cols = _table(page_table, "page_table")
+        _need(all(0 <= x < 1 << 31 for x in (total_q, max_new, max_len)), "total_q, max_new, max_len: 0 to 2^31 - 1")       # (fields of 32 bits would wrap)
         _need(kv_len.shape[0] == n and q_start.shape[0] == n + 1 and kv_len.is_contiguous() and q_start.is_contiguous(),
               f"kv_len: {n} contiguous values, q_start: {n + 1}")
         self.device, self.total_q = dev, int(total_q)

@@ -77,14 +77,18 @@ fd_status check_rotary(const Err& err, int head_dim, int rot, int layout, double
     if (!positions || !freqs) return err(FD_ERR_INVALID, "positions and freqs must be non-null");
     return FD_OK;
 }
+fd_status check_bounds(const Err& err, const fd_kv_batch* b) {
+    if (b->total_q < 0 || b->max_new < 0 || b->max_new > b->total_q || (b->max_new == 0 && b->total_q > 0) || b->max_len < 0) return err(FD_ERR_INVALID, "bad bounds: total_q %d, max_new %d, max_len %d", b->total_q, b->max_new, b->max_len);
+    if (b->max_len > (1 << 30) || b->total_q > (1 << 30)) return err(FD_ERR_UNSUPPORTED, "lengths up to 2^30 tokens are covered");
+    return FD_OK;
+}
 fd_status check_batch(const Err& err, const fd_kv* kv, const fd_kv_batch* b, bool queries) {
     if (!kv || !b) return err(FD_ERR_INVALID, "cache and batch must be non-null");
     if (b->batch < 0 || b->batch > 65535) return err(FD_ERR_INVALID, "batch = %d: 0 to 65535", b->batch);
     if (b->batch == 0) return FD_OK;
     if (!b->table_dev || !b->kv_len_dev || (queries && !b->q_start_dev)) return err(FD_ERR_INVALID, "page table, lengths and starts must be non-null");
     if (b->max_pages < 1 || b->table_stride < 0) return err(FD_ERR_INVALID, "bad page table: %d pages a row, stride %lld", b->max_pages, (long long)b->table_stride);
-    if (b->total_q < 0 || b->max_new < 0 || b->max_new > b->total_q || (b->max_new == 0 && b->total_q > 0) || b->max_len < 0) return err(FD_ERR_INVALID, "bad bounds: total_q %d, max_new %d, max_len %d", b->total_q, b->max_new, b->max_len);
-    if (b->max_len > (1 << 30) || b->total_q > (1 << 30)) return err(FD_ERR_UNSUPPORTED, "lengths up to 2^30 tokens are covered");
+    FD_TRY(check_bounds(err, b));
     return FD_OK;
 }
 Batch batch_of(const fd_kv* kv, const fd_kv_batch* b) {
@@ -302,7 +306,8 @@ fd_status fd_kv_append(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_append
 }
 
 size_t fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* b, int32_t q_heads, int32_t weights) {
-    if (!kv || !b || q_heads < 1 || q_heads % kv->d.heads || q_heads / kv->d.heads > 128 || b->batch < 1 || b->total_q < 1) return 0;
+    if (!kv || !b || q_heads < 1 || q_heads % kv->d.heads || q_heads / kv->d.heads > 128 || b->batch < 1 || b->batch > 65535 || b->total_q < 1) return 0;
+    if (check_bounds(Err(nullptr, 0), b) != FD_OK) return 0;
     return plan_attend(kv, b, q_heads, weights != 0).bytes();
 }
 

@@ -924,3 +924,24 @@ def test_totals_and_lengths_that_overlap_are_refused(fd):
     p.cache.attend(p.batch, q, weights=a, weights_out=a)
     assert torch.equal(totals[:120], totals[120:240]) and float(totals.sum()) > 0
     p.cache.synchronize()
+
+
+def test_attend_bytes_of_wrong_bounds(fd):
+    """0, as for every wrong argument: no workspace is taken for a call that will be refused."""
+    import ctypes
+    p = Pool(fd, 5, [300], [2], 2, 64, 16, FP16)
+    assert fd.lib.fd_kv_attend_bytes(p.cache._h, ctypes.byref(p.batch.struct), 4, 1) > 0
+    q, w = randn(6, 2, 4, 64, dtype=FP16), torch.zeros(1, 2, 300, device=DEV)
+    for name, value in (("max_len", -1), ("max_len", 2 ** 31 - 1), ("max_new", 3), ("max_new", -1), ("max_new", 0), ("batch", 70000)):
+        batch = fd.KVBatch(p.table, p.kv_len, p.q_start, 2, 2, 300)
+        setattr(batch.struct, name, value)
+        assert fd.lib.fd_kv_attend_bytes(p.cache._h, ctypes.byref(batch.struct), 4, 1) == 0, name
+        with pytest.raises(fd.FdError):
+            p.cache.attend(batch, q, weights=w)
+    batch = fd.KVBatch(p.table, p.kv_len, p.q_start, 2, 2, 300)
+    size = fd.lib.fd_kv_attend_bytes(p.cache._h, ctypes.byref(batch.struct), 4, 1)
+    batch.struct.table_dev = batch.struct.kv_len_dev = batch.struct.q_start_dev = None           # sizes are asked for before there are any arrays
+    assert fd.lib.fd_kv_attend_bytes(p.cache._h, ctypes.byref(batch.struct), 4, 1) == size
+    for total_q, max_new, max_len in ((2 ** 32 + 2, 2, 300), (2, 2 ** 32 + 2, 300), (2, 2, 2 ** 32 + 300), (-1, 0, 300)):
+        with pytest.raises(fd.FdError):
+            fd.KVBatch(p.table, p.kv_len, p.q_start, total_q, max_new, max_len)
