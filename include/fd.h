@@ -436,7 +436,7 @@ fd_status fd_kv_append(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_ap
  * null = zeros, and may be weights_out.  It needs lse_dev.  out must not overlap q. */
 typedef struct {
     fd_heads q, out;
-    double   scale;
+    double   scale;                            /* above 0; a normal fp32 number */
     int32_t  causal, window;
     float*   lse_dev;
     const float* weights_in_dev; float* weights_out_dev; int64_t weights_stride;

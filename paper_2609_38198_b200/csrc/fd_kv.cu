@@ -1,4 +1,5 @@
 // Entry points of the paged cache's operators and of rotary positions: argument checks, tensor maps, launches (fd.h: "kept keys and values").
+#include <float.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -334,6 +335,8 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
         if (!rows_apart(x->out, b->total_q, d.head_dim)) return err(FD_ERR_INVALID, "out: rows overlap");
     }
     if (!(x->scale > 0) || !(x->scale < 1e30)) return err(FD_ERR_INVALID, "scale must be positive");
+    // (a hidden score is -inf, and -inf times a scale that rounds to 0 is NaN)
+    if (!((float)(x->scale * kLog2e) >= FLT_MIN)) return err(FD_ERR_UNSUPPORTED, "scale = %g: below what fp32 holds as a normal number", x->scale);
     if (x->window < 0 || (x->window > 0 && !x->causal)) return err(FD_ERR_INVALID, "a window is positive and causal (0: none)");
     FD_TRY(check_device(err, kv));
     if (b->total_q == 0 && !x->weights_out_dev) return FD_OK;

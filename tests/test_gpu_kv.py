@@ -945,3 +945,13 @@ def test_attend_bytes_of_wrong_bounds(fd):
     for total_q, max_new, max_len in ((2 ** 32 + 2, 2, 300), (2, 2 ** 32 + 2, 300), (2, 2, 2 ** 32 + 300), (-1, 0, 300)):
         with pytest.raises(fd.FdError):
             fd.KVBatch(p.table, p.kv_len, p.q_start, total_q, max_new, max_len)
+
+
+def test_attend_smallest_scales(fd):
+    """A scale that is no normal fp32 number is refused (0 times the -inf of a hidden score is NaN); the smallest normal ones give means."""
+    p = Pool(fd, 5, [300, 300], [1, 40], 1, 64, 16, BF16)
+    q = randn(6, 41, 1, 64, dtype=BF16)
+    for scale in (1e-300, 1e-46, 1e-39):
+        with pytest.raises(fd.FdError):
+            p.cache.attend(p.batch, q, scale=scale)
+    check_attend(fd, p, q, scale=1e-37)
