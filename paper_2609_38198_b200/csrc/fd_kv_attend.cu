@@ -435,9 +435,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         if (ok && t < tiles && warp_on) {
             tc_fence_after();
             const bool empty = m == -INFINITY;
-            // The tensor core adds with truncation, the norm was summed with rounding: every addition of 16 tokens into the accumulator loses 2.98e-8 of it on average,
-            // which is added back.  (Where all products have one sign it loses 1e-7, for which a cache is cut into parts of kPartTokens.)
-            const float inv = empty ? 0.f : (1.0f + (float)num * (8 * 2.98023224e-8f)) / l;
+            // (the tensor core adds with truncation: see kPartTokens)
+            const float inv = empty ? 0.f : 1.0f / l;
             const int64_t row = w.begin + token;
             const bool odd = num > 0 && *(volatile int*)&bars->odd;
             if (valid) {

@@ -955,3 +955,24 @@ def test_attend_smallest_scales(fd):
         with pytest.raises(fd.FdError):
             p.cache.attend(p.batch, q, scale=scale)
     check_attend(fd, p, q, scale=1e-37)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("new", [1, 40])
+def test_attend_concentrated_rows_are_not_scaled(fd, dtype, new):
+    """Two equal weights far above 32766 others: the result is the mean of two neighbouring numbers, a tie that goes to the even one.  Anything that multiplies the
+    result by more than 1 makes it the odd one."""
+    n, dim = 32768, 64
+    k = torch.zeros(n // 64, 64, 1, dim, dtype=dtype, device=DEV)
+    v = torch.zeros(n // 64, 64, 1, dim, dtype=dtype, device=DEV)
+    k[3, 5, 0, 0] = k[400, 7, 0, 0] = 16.0
+    v[3, 5] = 1.0
+    v[400, 7] = 1.0 + torch.finfo(dtype).eps
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    cache = fd.KVCache(k, v)
+    batch = fd.KVBatch(torch.arange(n // 64, dtype=torch.int32, device=DEV)[None], i32(n), i32(0, new), new, new, n)
+    q = torch.zeros(new, 1, dim, dtype=dtype, device=DEV)
+    q[..., 0] = 128.0                                        # in powers of two, all exact: scores of 256 and 0
+    out, _ = cache.attend(batch, q, scale=math.log(2.0) / 8, causal=False)
+    cache.synchronize()
+    assert (out == 1.0).all()
