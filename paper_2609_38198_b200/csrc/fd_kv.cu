@@ -149,6 +149,8 @@ Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weight
         p.parts = (size_t)round_up(2 * (int64_t)b->batch * heads, 4);
         p.part_o = (size_t)2 * p.ctas * kFewRows * dim;
         p.part_lse = (size_t)2 * p.ctas * kFewRows;
+        // (a warp's tokens of a cache: a quarter of it, and the rest of a chunk)
+        if (b->max_len >= kFewWarps * kPartTokens) p.folds = (size_t)p.ctas * kFewWarps * (dim / 8 + 1) * 32 * 4;
         if (weights) {
             p.score_stride = round_up(b->max_len, 64);
             p.scores = (size_t)b->batch * heads * b->max_new * group * p.score_stride;
@@ -365,6 +367,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
         a.part_o = static_cast<float*>(workspace_dev) + p.parts;
         a.part_lse = a.part_o + p.part_o;
         a.scores = p.scores ? a.part_lse + p.part_lse : nullptr; a.score_stride = p.score_stride;
+        a.folds = p.folds ? a.part_lse + p.part_lse + p.scores : nullptr;
         a.q = heads_of(x->q);
         cudaError_t e;
         if (few) {

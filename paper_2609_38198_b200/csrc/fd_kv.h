@@ -105,13 +105,15 @@ struct AttendArgs {
     int2* parts;                     // (sequence, head)
     float* part_o; float* part_lse;  // [split][token][query head]([head_dim]); few rows: [slot][kFewRows]([head_dim])
     float* scores; int64_t score_stride;     // few rows and weights: scale_log2 q.k of every row and slot, [sequence][head][few_rows][score_stride]
+    float* folds;                    // few rows, caches that fill an accumulator more than once: sums of every warp
     int box_rows;
     const void* v_pool; int64_t v_page, v_token, v_head;
 };
 // At most this many rows (new tokens x query heads of a group) of a sequence go through the kernel for few rows.
 constexpr int kFewRows = 16;
+constexpr int kFewWarps = 4;             // warps of a CTA of that kernel; each goes through a quarter of what the CTA has of a cache
 constexpr int kMaxSplits = 1024;         // parts of a cache
-// Longest stretch of tokens that one accumulator in tensor memory sums.  The tensor core truncates: of values of one sign, 1e-7 of the sum is lost with every 16
+// Longest stretch of tokens that one accumulator of matrix products sums.  The tensor core truncates: of values of one sign, 1e-7 of the sum is lost with every 16
 // tokens (262144 tokens: 1.7e-3, nearly four half steps of fp16); parts are joined with rounding, so the loss ends at 2e-4.
 constexpr int kPartTokens = 32768;
 
@@ -120,8 +122,8 @@ struct Plan {
     bool few;
     int row_tiles, splits, split_tiles, ctas;
     int64_t score_stride;
-    size_t parts, part_o, part_lse, scores;         // in floats, in this order, each a multiple of 4
-    size_t bytes() const { return (parts + part_o + part_lse + scores) * sizeof(float); }
+    size_t parts, part_o, part_lse, scores, folds;  // in floats, in this order, each a multiple of 4
+    size_t bytes() const { return (parts + part_o + part_lse + scores + folds) * sizeof(float); }
 };
 Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weights);
 cudaError_t launch_attend(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream);

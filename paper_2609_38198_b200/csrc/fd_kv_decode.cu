@@ -18,7 +18,7 @@ namespace fd {
 namespace kv {
 namespace {
 
-constexpr int kWarpsFew = 4;
+constexpr int kWarpsFew = kFewWarps;
 // (see Elem; raising the maximum costs little beside the cache's bytes)
 template <class T> constexpr float kLazy = 8.f;
 template <> constexpr float kLazy<__half> = 3.f;
@@ -215,6 +215,33 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
         bool odd = false;
 
+        // Accumulators that a warp has filled with kPartTokens tokens (mma.sync truncates as tcgen05 does) are added to fp32 sums in the workspace, with rounding and at
+        // the maximum of the moment; each thread has its own.  first: nothing is there yet; last: the sums come back into the registers.
+        auto fold = [&](bool first, bool last) {
+            float4* f = (float4*)a.folds + ((int64_t)(blockIdx.x * kWarpsFew + warp) * (D / 8 + 1)) * 32 + lane;
+            if (!first) {
+                const float4 z = f[D / 8 * 32];
+                const float fa[2] = {z.x == m[0] ? 1.0f : ex2f((z.x - m[0]) * c), z.y == m[1] ? 1.0f : ex2f((z.y - m[1]) * c)};
+                l[0] = fmaf(fa[0], z.z, l[0]);
+                l[1] = fmaf(fa[1], z.w, l[1]);
+#pragma unroll
+                for (int n = 0; n < D / 8; ++n) {
+                    const float4 y = f[n * 32];
+                    o[n][0] = fmaf(fa[0], y.x, o[n][0]); o[n][1] = fmaf(fa[0], y.y, o[n][1]);
+                    o[n][2] = fmaf(fa[1], y.z, o[n][2]); o[n][3] = fmaf(fa[1], y.w, o[n][3]);
+                }
+            }
+            if (last) return;
+            f[D / 8 * 32] = make_float4(m[0], m[1], l[0], l[1]);
+            l[0] = l[1] = 0.f;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) {
+                f[n * 32] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+                o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+            }
+        };
+        constexpr int kFold = kPartTokens / KEYS;
+
         int i = 0;
         for (; i < mine; ++i) {
             const int st = (done + i) % G::kStages, key = (c0 + warp + kWarpsFew * i) * KEYS;
@@ -299,7 +326,9 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
             }
             __syncwarp();
             if (i + G::kStages < mine) issue(i + G::kStages);
+            if ((i + 1) % kFold == 0 && i + 1 < mine && a.folds) fold(i + 1 == kFold, false);
         }
+        if (ok && mine > kFold && a.folds) fold(false, true);
         if (!ok && lane == 0) {                      // aborted: copies in flight land before the CTA exits (bounded)
             for (int k = i; k < min(i + G::kStages, mine); ++k) {
                 const long long t0 = clock64();

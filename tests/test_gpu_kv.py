@@ -976,3 +976,61 @@ def test_attend_concentrated_rows_are_not_scaled(fd, dtype, new):
     out, _ = cache.attend(batch, q, scale=math.log(2.0) / 8, causal=False)
     cache.synchronize()
     assert (out == 1.0).all()
+
+
+@pytest.mark.parametrize("dtype", [FP16, BF16])
+def test_attend_long_sums_of_one_sign_few_rows(fd, dtype):
+    """As test_attend_long_sums_of_one_sign for one new token: 296 caches of 2^20 tokens (37 sequences read the same pages), so that a warp goes through 262144."""
+    n, batch, heads, dim = 1 << 20, 37, 8, 64
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k = (torch.randn(n // 64, 64, heads, dim, device=DEV, generator=g) * 0.5).to(dtype)
+    v = (1 + torch.rand(dim, device=DEV, generator=g) + 0.1 * torch.rand(n // 64, 64, heads, dim, device=DEV, generator=g)).to(dtype)
+    table = torch.arange(n // 64, dtype=torch.int32, device=DEV)[None].repeat(batch, 1)
+    cache = fd.KVCache(k, v)
+    kv_len = torch.full((batch,), n, dtype=torch.int32, device=DEV)
+    q = torch.randn(batch, heads, dim, device=DEV, generator=g).to(dtype)
+    out, lse = cache.attend(fd.KVBatch(table, kv_len, torch.arange(batch + 1, dtype=torch.int32, device=DEV), batch, 1, n), q)
+    cache.synchronize()
+    for h in (0, heads - 1):
+        s = q[:, h].double() @ k[:, :, h].reshape(n, dim).double().T / 8
+        want = torch.softmax(s, -1) @ v[:, :, h].reshape(n, dim).double()
+        # (a mean over 37 x 64 results, whose own roundings average out)
+        assert abs(float((out[:, h].double() / want - 1).mean())) <= 2.0 ** -12, float((out[:, h].double() / want - 1).mean())
+        # 1024 additions of much the same size, each off by half a step of what is there or less; the exponentials, the logarithm and the largest score
+        assert (lse[:, h].double() - torch.logsumexp(s, -1)).abs().max() <= 512 * 2.0 ** -24 + 2.0 ** -22 * (8 + 16)
+
+
+@pytest.mark.parametrize("rising", [True, False])
+def test_attend_few_rows_over_long_caches(fd, rising):
+    """Caches that fill a warp's accumulators several times (296 of 300032 tokens, the pages shared), with scores that rise or fall along the cache, two new tokens
+    and two query heads a cached head."""
+    n, batch, heads, dim, new, group = 300032, 37, 8, 128, 2, 2
+    g = torch.Generator(device=DEV).manual_seed(2)
+    size = torch.linspace(0.1, 2.0, n, device=DEV)
+    k = torch.randn(n, heads, dim, device=DEV, generator=g) * (size if rising else size.flip(0))[:, None, None]
+    k = k.to(BF16).view(n // 64, 64, heads, dim)
+    v = torch.randn(n // 64, 64, heads, dim, device=DEV, generator=g).to(BF16)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    cache = fd.KVCache(k, v)
+    table = torch.arange(n // 64, dtype=torch.int32, device=DEV)[None].expand(batch, -1)
+    q = torch.randn(batch * new, heads * group, dim, device=DEV, generator=g).to(BF16)
+    w = torch.zeros(batch, heads, n, device=DEV)
+    out, lse = cache.attend(fd.KVBatch(table, i32([n] * batch), i32([new * b for b in range(batch + 1)]), batch * new, new, n), q, weights=w)
+    cache.synchronize()
+    for b, h in ((0, 0), (17, 5), (36, 7)):
+        x = q[new * b:new * (b + 1), group * h:group * (h + 1)].double()                         # [new, group, dim]
+        kk, vv = k[:, :, h].reshape(n, dim).double(), v[:, :, h].reshape(n, dim).double()
+        s = torch.einsum("igd,jd->igj", x, kk) * dim ** -0.5
+        s[0, :, n - 1] = -math.inf
+        p = torch.softmax(s, -1)
+        want, size_ = p @ vv, p @ vv.abs()
+        top = float(s[s > -math.inf].abs().max())
+        sure = 2.0 ** -19 * dim ** -0.5 * float((x.abs() @ kk.abs().T).max()) + 2.0 ** -22 * (8 + top)
+        got = out[new * b:new * (b + 1), group * h:group * (h + 1)].double()
+        # (2^-12 of the sum of magnitudes for the truncation of 32768 tokens)
+        tol = (2.0 ** -8 + 2 * sure + 2.0 ** -12) * size_ + 2.0 ** -8 * want.abs()
+        assert ((got - want).abs() <= tol).all(), float(((got - want).abs() / tol).max())
+        e = lse[new * b:new * (b + 1), group * h:group * (h + 1)].double() - torch.logsumexp(s, -1)
+        assert e.abs().max() <= 2 * sure + 512 * 2.0 ** -24
+        total = p.sum((0, 1))
+        assert ((w[b, h].double() - total).abs() <= total * (2 * sure + 512 * 2.0 ** -24 + 2.0 ** -20 * (1 + 40)) + 2.0 ** -140).all()
