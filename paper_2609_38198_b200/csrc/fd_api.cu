@@ -10,7 +10,7 @@
 
 namespace fd {
 
-int64_t g_launches = 0;
+std::atomic<int64_t> g_launches{0};
 
 fd_status fail(fd_ctx* c, fd_status st, const char* fmt, ...) {
     if (c) {

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 #include <stddef.h>
+#include <atomic>
 #include <string>
 
 #include "fd.h"
@@ -127,7 +128,7 @@ struct fd_ctx {
 
 namespace fd {
 
-extern int64_t g_launches;           // kernels launched by this library in this process
+extern std::atomic<int64_t> g_launches;       // kernels launched by this library in this process, by any of its threads
 
 fd_status fail(fd_ctx* c, fd_status st, const char* fmt, ...);
 fd_status cuda_fail(fd_ctx* c, cudaError_t e, const char* what);

@@ -1034,3 +1034,35 @@ def test_attend_few_rows_over_long_caches(fd, rising):
         assert e.abs().max() <= 2 * sure + 512 * 2.0 ** -24
         total = p.sum((0, 1))
         assert ((w[b, h].double() - total).abs() <= total * (2 * sure + 512 * 2.0 ** -24 + 2.0 ** -20 * (1 + 40)) + 2.0 ** -140).all()
+
+
+def test_calls_from_several_threads(fd):
+    """One cache, its calls from four threads on streams of their own: every result, and every launch counted."""
+    import threading
+    p = Pool(fd, 5, [300], [1], 2, 64, 16, BF16)
+    q = randn(6, 1, 4, 64, dtype=BF16)
+    ref, ref_lse = p.cache.attend(p.batch, q)
+    pos, freqs = torch.zeros(1, dtype=torch.int32, device=DEV), fd.fd_rotary_frequencies(64, device=DEV)
+    before = fd.fd_launch_count()
+    p.cache.attend(p.batch, q)
+    each = fd.fd_launch_count() - before + 1                # (and one for the rotation)
+    torch.cuda.synchronize()
+    wrong, calls, threads = [], 500, 4
+
+    def work():
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(calls):
+                fd.fd_rotary(q, pos, freqs)
+                out, lse = p.cache.attend(p.batch, q)
+            if not (torch.equal(out, ref) and torch.equal(lse, ref_lse)):
+                wrong.append(1)
+
+    before = fd.fd_launch_count()
+    all_ = [threading.Thread(target=work) for _ in range(threads)]
+    for t in all_:
+        t.start()
+    for t in all_:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong and fd.fd_launch_count() - before == threads * calls * each
+    p.cache.synchronize()
