@@ -351,7 +351,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
     a.scale_log2 = (float)(x->scale * kLog2e);
     a.lse = x->lse_dev;
     a.w_in = x->weights_in_dev; a.w_out = x->weights_out_dev; a.w_stride = x->weights_stride;
-    a.box_rows = kv->box_rows;
+    a.box_rows = kv->box_rows; a.sm_count = kv->sm_count;
     a.v_pool = d.v_dev; a.v_page = d.v_page_stride; a.v_token = d.v_token_stride; a.v_head = d.v_head_stride;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     CUtensorMap mq;

@@ -101,6 +101,7 @@ struct AttendArgs {
     const float* w_in; float* w_out; int64_t w_stride;
     int row_tiles;                   // many rows: tiles of 128 rows a CTA
     int splits, split_tiles;         // many rows: the cache in `splits` parts of split_tiles tiles of 128 tokens
+    int sm_count;
     int ctas, few_rows;              // few rows: CTAs that share the batch's caches; rows a sequence has at most; first CTA and number of the parts of each
     int2* parts;                     // (sequence, head)
     float* part_o; float* part_lse;  // [split][token][query head]([head_dim]); few rows: [slot][kFewRows]([head_dim])

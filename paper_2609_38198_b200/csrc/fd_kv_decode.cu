@@ -541,7 +541,7 @@ cudaError_t few_t(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap&
     ++g_launches;
     if ((e = launch_behind(stream, dim3((unsigned)a.ctas), dim3(kWarpsFew * 32), GeoFew<D>::kSmem, k_few<T, D>, mk, mv, a)) != cudaSuccess) return e;
     const int64_t caches = (int64_t)a.batch.batch * a.heads, join = a.ctas > 1 ? caches * a.few_rows : 0;
-    const int64_t per = a.w_out ? std::min<int64_t>(ceil_div(a.batch.max_len, kWeighTokens), std::max<int64_t>(1, ceil_div(16 * 148, caches))) : 0, weigh = per * caches;
+    const int64_t per = a.w_out ? std::min<int64_t>(ceil_div(a.batch.max_len, kWeighTokens), std::max<int64_t>(1, ceil_div(16 * (int64_t)a.sm_count, caches))) : 0, weigh = per * caches;
     if (weigh + join > INT32_MAX) return cudaErrorInvalidConfiguration;
     if (weigh + join == 0) return cudaSuccess;
     ++g_launches;
