@@ -446,7 +446,7 @@ size_t    fd_kv_attend_bytes(const fd_kv* kv, const fd_kv_batch* batch, int32_t 
 fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_attend_args* args, void* workspace_dev,
                        size_t workspace_bytes, void* cuda_stream, char* errbuf, size_t errbuf_len);
 
-/* Eviction: of every sequence longer than `keep`, each head keeps its first `first` tokens, its last `recent` ones and, of those between, the
+/* Eviction: of every sequence longer than `keep` (up to 2^30), each head keeps its first `first` tokens, its last `recent` ones and, of those between, the
  * ones with the largest weights (of equal ones the earlier; a NaN counts as the smallest), `keep` in all and in their order: row r
  * of the new cache is the old slot kept[r].  new_table: the pages they move to, either the same pages in the same order as the batch's table
  * (in place; then no other sequence may share them) or pages that no sequence of the batch uses; ceil(keep / page_size) columns suffice.  kept_dev: [batch][heads][keep], -1 behind the last.  new_len_dev:

@@ -400,6 +400,7 @@ fd_status fd_kv_evict(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_evict_a
     const fd_kv_desc& d = kv->d;
     if (!x->weights_in_dev || !x->weights_out_dev || !x->kept_dev || !x->new_len_dev || !x->new_table_dev) return err(FD_ERR_INVALID, "weights, kept, new_len and new_table must be non-null");
     if (x->keep < 1 || x->first < 0 || x->recent < 0 || (int64_t)x->first + x->recent > x->keep) return err(FD_ERR_INVALID, "keep = %d, first = %d, recent = %d", x->keep, x->first, x->recent);
+    if (x->keep > (1 << 30)) return err(FD_ERR_UNSUPPORTED, "keep = %d: lengths up to 2^30 tokens are covered", x->keep);
     if (x->weights_stride < b->max_len) return err(FD_ERR_INVALID, "weights: stride %lld is below max_len = %d", (long long)x->weights_stride, b->max_len);
     if (partly_over(x->weights_in_dev, x->weights_out_dev, (int64_t)b->batch * d.heads, x->weights_stride, b->max_len))
         return err(FD_ERR_INVALID, "weights_out overlaps weights_in without being it");

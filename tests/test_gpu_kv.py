@@ -1066,3 +1066,16 @@ def test_calls_from_several_threads(fd):
     torch.cuda.synchronize()
     assert not wrong and fd.fd_launch_count() - before == threads * calls * each
     p.cache.synchronize()
+
+
+def test_evict_keeps_no_more_than_lengths_reach(fd):
+    """keep beyond 2^30, the longest length, is refused: loops over `keep` slots in 32 bits would run over."""
+    import ctypes
+    from paper_2609_38198_b200 import binding as b
+    p = Pool(fd, 5, [30], [0], 2, 64, 16, BF16)
+    w = torch.zeros(1, 2, 30, device=DEV)
+    for keep in ((1 << 30) + 1, 2 ** 31 - 1):
+        x = b.fd_kv_evict_args(w.data_ptr(), w.data_ptr(), 30, p.table.data_ptr(), p.cols, p.cols, keep, 0, 0, w.data_ptr(), p.kv_len.data_ptr())
+        launches = fd.fd_launch_count()
+        assert b.lib.fd_kv_evict(p.cache._h, ctypes.byref(p.batch.struct), ctypes.byref(x), None, None, 0) == fd.FD_ERR_UNSUPPORTED
+        assert fd.fd_launch_count() == launches
