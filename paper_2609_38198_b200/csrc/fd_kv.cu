@@ -54,6 +54,8 @@ bool make_map(CUtensorMap* m, void* base, int dtype, int rank, const uint64_t* d
 
 constexpr int64_t kMaxStride = (int64_t)1 << 38;      // (a tensor map's strides end at 2^40 bytes)
 
+bool misaligned(const void* p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size != 0; }
+
 // A tensor of heads that is read or written in vectors of 16 bytes, or by TMA.
 fd_status check_wide(const Err& err, const fd_heads& h, int head_dim, const char* what) {
     if (!h.p_dev || h.heads < 1) return err(FD_ERR_INVALID, "%s: no tensor", what);
@@ -67,7 +69,7 @@ fd_status check_rows(const Err& err, const fd_heads& h, int head_dim, int size, 
     if (!h.p_dev || h.heads < 1) return err(FD_ERR_INVALID, "%s: no tensor", what);
     if (h.token_stride < 0 || h.head_stride < 0 || h.token_stride > kMaxStride || h.head_stride > kMaxStride || (h.heads > 1 && h.head_stride < head_dim))
         return err(FD_ERR_INVALID, "%s: bad strides", what);
-    if (reinterpret_cast<uintptr_t>(h.p_dev) % size) return err(FD_ERR_INVALID, "%s: misaligned pointer", what);
+    if (misaligned(h.p_dev, size)) return err(FD_ERR_INVALID, "%s: misaligned pointer", what);
     return FD_OK;
 }
 fd_status check_rotary(const Err& err, int head_dim, int rot, int layout, double scale, const void* positions, const void* freqs) {
@@ -76,6 +78,7 @@ fd_status check_rotary(const Err& err, int head_dim, int rot, int layout, double
     if (layout != FD_ROTARY_HALF && layout != FD_ROTARY_INTERLEAVED) return err(FD_ERR_INVALID, "unknown layout %d", layout);
     if (!(fabs(scale) <= 3e38)) return err(FD_ERR_INVALID, "scale is not finite");
     if (!positions || !freqs) return err(FD_ERR_INVALID, "positions and freqs must be non-null");
+    if (misaligned(positions, 4) || misaligned(freqs, 8)) return err(FD_ERR_INVALID, "positions or freqs: misaligned pointer");
     return FD_OK;
 }
 fd_status check_bounds(const Err& err, const fd_kv_batch* b) {
@@ -88,6 +91,7 @@ fd_status check_batch(const Err& err, const fd_kv* kv, const fd_kv_batch* b, boo
     if (b->batch < 0 || b->batch > 65535) return err(FD_ERR_INVALID, "batch = %d: 0 to 65535", b->batch);
     if (b->batch == 0) return FD_OK;
     if (!b->table_dev || !b->kv_len_dev || (queries && !b->q_start_dev)) return err(FD_ERR_INVALID, "page table, lengths and starts must be non-null");
+    if (misaligned(b->table_dev, 4) || misaligned(b->kv_len_dev, 4) || (queries && misaligned(b->q_start_dev, 4))) return err(FD_ERR_INVALID, "page table, lengths or starts: misaligned pointer");
     if (b->max_pages < 1 || b->table_stride < 0) return err(FD_ERR_INVALID, "bad page table: %d pages a row, stride %lld", b->max_pages, (long long)b->table_stride);
     FD_TRY(check_bounds(err, b));
     return FD_OK;
@@ -321,6 +325,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_attend
     if (!x) return err(FD_ERR_INVALID, "arguments must be non-null");
     if (b->batch == 0) return FD_OK;
     const fd_kv_desc& d = kv->d;
+    if (misaligned(x->lse_dev, 4) || misaligned(x->weights_in_dev, 4) || misaligned(x->weights_out_dev, 4)) return err(FD_ERR_INVALID, "lse or weights: misaligned pointer");
     if (x->weights_out_dev) {
         if (!x->lse_dev && b->total_q > 0) return err(FD_ERR_INVALID, "weights need lse");
         if (x->weights_stride < b->max_len) return err(FD_ERR_INVALID, "weights: stride %lld is below max_len = %d", (long long)x->weights_stride, b->max_len);
@@ -399,6 +404,8 @@ fd_status fd_kv_evict(const fd_kv* kv, const fd_kv_batch* b, const fd_kv_evict_a
     if (b->batch == 0) return FD_OK;
     const fd_kv_desc& d = kv->d;
     if (!x->weights_in_dev || !x->weights_out_dev || !x->kept_dev || !x->new_len_dev || !x->new_table_dev) return err(FD_ERR_INVALID, "weights, kept, new_len and new_table must be non-null");
+    for (const void* p : {(const void*)x->weights_in_dev, (const void*)x->weights_out_dev, (const void*)x->kept_dev, (const void*)x->new_len_dev, (const void*)x->new_table_dev})
+        if (misaligned(p, 4)) return err(FD_ERR_INVALID, "weights, kept, new_len or new_table: misaligned pointer");
     if (x->keep < 1 || x->first < 0 || x->recent < 0 || (int64_t)x->first + x->recent > x->keep) return err(FD_ERR_INVALID, "keep = %d, first = %d, recent = %d", x->keep, x->first, x->recent);
     if (x->keep > (1 << 30)) return err(FD_ERR_UNSUPPORTED, "keep = %d: lengths up to 2^30 tokens are covered", x->keep);
     if (x->weights_stride < b->max_len) return err(FD_ERR_INVALID, "weights: stride %lld is below max_len = %d", (long long)x->weights_stride, b->max_len);

@@ -1079,3 +1079,36 @@ def test_evict_keeps_no_more_than_lengths_reach(fd):
         launches = fd.fd_launch_count()
         assert b.lib.fd_kv_evict(p.cache._h, ctypes.byref(p.batch.struct), ctypes.byref(x), None, None, 0) == fd.FD_ERR_UNSUPPORTED
         assert fd.fd_launch_count() == launches
+
+
+def test_misaligned_arrays_are_refused(fd):
+    """Arrays that do not lie on a multiple of their element, through the C entry points: refused before anything is launched."""
+    import ctypes
+    from paper_2609_38198_b200 import binding as b
+    p = Pool(fd, 5, [30], [2], 2, 64, 16, BF16)
+    w = torch.zeros(1, 2, 30, device=DEV)
+    t = torch.zeros(2, 2, 64, dtype=BF16, device=DEV)
+    o = torch.zeros(2, 2, 64, dtype=BF16, device=DEV)
+    h, ho = b.fd_heads(t.data_ptr(), 128, 64, 2), b.fd_heads(o.data_ptr(), 128, 64, 2)
+    pos, freqs = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(40, dtype=torch.float64, device=DEV)
+    null = b.fd_heads(None, 0, 0, 0)
+    launches = fd.fd_launch_count()
+
+    def refused(entry, args, *more):
+        err = ctypes.create_string_buffer(256)
+        assert entry(p.cache._h, ctypes.byref(p.batch.struct), ctypes.byref(args), *more, None, err, 256) == fd.FD_ERR_INVALID and b"misaligned" in err.value
+
+    for dp, df in ((2, 0), (0, 4)):
+        refused(b.lib.fd_kv_append, b.fd_kv_append_args(h, h, null, null, pos.data_ptr() + dp, freqs.data_ptr() + df, 1.0, 64, 0))
+    for dl, di, do in ((2, 0, 0), (0, 1, 0), (0, 0, 2)):
+        refused(b.lib.fd_kv_attend, b.fd_kv_attend_args(h, ho, 1.0, 1, 0, w.data_ptr() + dl, w.data_ptr() + di, w.data_ptr() + do, 30), None, 0)
+    for i in range(5):
+        d = [2 * (j == i) for j in range(5)]
+        refused(b.lib.fd_kv_evict, b.fd_kv_evict_args(w.data_ptr() + d[0], w.data_ptr() + d[1], 30, p.table.data_ptr() + d[2], p.cols, p.cols, 10, 0, 0,
+                                                      w.data_ptr() + d[3], p.kv_len.data_ptr() + d[4]))
+    for name in ("table_dev", "kv_len_dev", "q_start_dev"):
+        whole = getattr(p.batch.struct, name)
+        setattr(p.batch.struct, name, whole + 2)
+        refused(b.lib.fd_kv_append, b.fd_kv_append_args(h, h, null, null, None, None, 1.0, 0, 0))
+        setattr(p.batch.struct, name, whole)
+    assert fd.fd_launch_count() == launches

@@ -142,3 +142,8 @@ def test_results_whose_rows_overlap_are_refused(fd, tokens, heads):
                                   None, err, 256)
             assert st == fd.FD_ERR_INVALID and err.value == (b"out overlaps x without being x" if apart else b"out: rows overlap"), (ts, hs)
     assert fd.fd_launch_count() == 0
+
+
+@pytest.mark.parametrize("kw", [dict(positions=258), dict(freqs=516)])
+def test_rotary_refuses_misaligned_arrays(fd, kw):
+    test_rotary_refuses(fd, kw, fd.FD_ERR_INVALID)
