@@ -359,8 +359,8 @@ fd_status fd_unit_peaks(void* scratch_dev, size_t scratch_bytes, void* cuda_stre
  *   Rows before q_start[0] (of sequences that another call takes) and from q_start[batch] on (padding) are neither read into a result nor written.
  *   All three arrays are read on the device, so a captured call takes its lengths at replay; total_q, max_new and max_len are
  *   upper bounds that size the launch.  A page number outside the pool, or a length outside [0, min(max_len,
- *   max_pages * page_size)], is never followed: the tokens of such a page count as zeros, the length is clamped; appends write neither
- *   to such a page nor any token of a sequence with such a length; and fd_kv_synchronize reports FD_ERR_INVALID.  max_new chooses attention's kernel: where
+ *   max_pages * page_size)], is never followed: the tokens of such a page count as zeros, attention clamps the length; appends write neither
+ *   to such a page nor any token of a sequence with such a length, which evictions leave as it is; and fd_kv_synchronize reports FD_ERR_INVALID.  max_new chooses attention's kernel: where
  *   max_new times the query heads of a cached head is 16 or less, a sequence with more new tokens counts as having none and is reported likewise.
  * Positions: angles are taken in fp64 as position * freqs[i] and reduced there, so far positions lose nothing.
  * Masks: new token i of a sequence stands at slot p = kv_len - new + i.  Causal: it sees slots <= p; window > 0: of these
@@ -451,7 +451,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_at
  * of the new cache is the old slot kept[r].  new_table: the pages they move to, either the same pages in the same order as the batch's table
  * (in place; then no other sequence may share them) or pages that no sequence of the batch uses; ceil(keep / page_size) columns suffice.  kept_dev: [batch][heads][keep], -1 behind the last.  new_len_dev:
  * [batch], may be kv_len.  weights_out_dev: the kept weights in their new order, zeros behind them up to kv_len; may be weights_in.
- * q_start is not read. */
+ * A sequence whose length is out of range keeps its pages, its weights and its length, and has -1 in kept.  q_start is not read. */
 typedef struct {
     const float* weights_in_dev; float* weights_out_dev; int64_t weights_stride;
     const int32_t* new_table_dev; int64_t new_table_stride; int32_t new_max_pages;

@@ -199,8 +199,9 @@ __global__ void __launch_bounds__(kSelThreads) k_select(const EvictArgs a) {
     const int n = kv_length(a.batch, b, true);
     const int64_t row = (int64_t)b * a.heads + h;
     int* kept = a.kept + row * a.keep;
-    if (n <= a.keep) {
-        for (int i = tid; i < a.keep; i += kSelThreads) kept[i] = i < n ? i : -1;
+    const bool whole = n == a.batch.kv_len[b];               // (a length that kv_length had to cut: nothing is kept, moved or counted, so that nothing is lost)
+    if (n <= a.keep || !whole) {
+        for (int i = tid; i < a.keep; i += kSelThreads) kept[i] = whole && i < n ? i : -1;
         return;
     }
     const int lo = a.first, hi = n - a.recent, len = hi - lo;            // (first + recent <= keep < n)
@@ -336,8 +337,9 @@ __global__ void __launch_bounds__(kMoveThreads) k_move(const EvictArgs a, const 
     const Batch& B = a.batch;
     const int* kept = a.kept + ((int64_t)b * a.heads + h) * a.keep;
     if ((int)blockIdx.x == 2 * shares) {
-        const int n = kv_length(B, b, false), count = min(n, a.keep);
-        if (write_len && h == 0 && threadIdx.x == 0) a.new_len[b] = count;
+        const int n = kv_length(B, b, false), raw = B.kv_len[b], count = min(n, a.keep);
+        if (write_len && h == 0 && threadIdx.x == 0) a.new_len[b] = n == raw ? count : raw;
+        if (n != raw) return;
         const float* w = a.w_in + ((int64_t)b * a.heads + h) * a.w_stride;
         float* out = a.w_out + ((int64_t)b * a.heads + h) * a.w_stride;
         constexpr int kDeep = 4;
@@ -376,7 +378,9 @@ __global__ void __launch_bounds__(kMoveThreads) k_move(const EvictArgs a, const 
 __global__ void k_new_len(const EvictArgs a) {
     grid_wait();
     const int b = blockIdx.x * blockDim.x + threadIdx.x;
-    if (b < a.batch.batch) a.new_len[b] = min(kv_length(a.batch, b, false), a.keep);
+    if (b >= a.batch.batch) return;
+    const int n = kv_length(a.batch, b, false);
+    if (n == a.batch.kv_len[b]) a.new_len[b] = min(n, a.keep);
 }
 
 }  // namespace

@@ -1112,3 +1112,34 @@ def test_misaligned_arrays_are_refused(fd):
         refused(b.lib.fd_kv_append, b.fd_kv_append_args(h, h, null, null, None, None, 1.0, 0, 0))
         setattr(p.batch.struct, name, whole)
     assert fd.fd_launch_count() == launches
+
+
+@pytest.mark.parametrize("how", ["bound", "table", "negative"])
+@pytest.mark.parametrize("over", [False, True])
+def test_evict_beyond_the_bounds_loses_nothing(fd, how, over):
+    """A sequence whose length is out of range is left alone and reported: cut to the bound, its newest tokens would be gone."""
+    p = Pool(fd, 5, [300, 290], [0, 0], 2, 64, 16, BF16)
+    w = torch.rand(2, 2, 400, device=DEV)
+    bound = 400
+    if how == "bound":
+        bound = 299
+    if how == "table":
+        p.kv_len[0] = p.cols * 16 + 1
+    if how == "negative":
+        p.kv_len[0] = -1
+    batch = fd.KVBatch(p.table, p.kv_len, p.q_start, 0, 0, bound)
+    wrong = int(p.kv_len[0])
+    old = [p.rows(b) for b in range(2)]
+    w0 = w.clone()
+    kept, new_len, _ = p.cache.evict(batch, w, 100, first=2, recent=30, new_len=p.kv_len if over else None)
+    with pytest.raises(fd.FdError) as e:
+        p.cache.synchronize()
+    assert e.value.status == fd.FD_ERR_INVALID
+    assert new_len.tolist() == [wrong, 100] and (kept[0] == -1).all() and torch.equal(w[0], w0[0])
+    now = p.rows(0)
+    assert torch.equal(now[0], old[0][0]) and torch.equal(now[1], old[0][1])
+    for h in range(2):                                       # the other sequence, as ever
+        want = torch.from_numpy(evict_plain(w0[1, h, :290].cpu().numpy(), 290, 100, 2, 30)).to(DEV)
+        assert torch.equal(kept[1, h].long(), want)
+        pg, r = p.where(1, torch.arange(100, device=DEV))
+        assert torch.equal(p.k[pg, r, h].double(), old[1][0][want, h]) and torch.equal(w[1, h, :100], w0[1, h, want])
