@@ -433,7 +433,7 @@ fd_status fd_kv_append(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_ap
  * multiple (up to 128) of the cache's heads, query head h reads head h / (q_heads / heads).  lse_dev (optional): [total_q][q_heads], the natural
  * logarithm of sum_j exp(scale q.k_j).  weights_out_dev (optional; [batch][heads][weights_stride] for both): weights_in + the sum over
  * new tokens and query heads of the softmax weight a slot received, for slots below kv_len (others are left alone); weights_in
- * null = zeros, and may be weights_out.  It needs lse_dev.  out must not overlap q. */
+ * null = zeros, and may be weights_out, but not lie partly over it.  It needs lse_dev.  out must not overlap q, nor two rows of it each other. */
 typedef struct {
     fd_heads q, out;
     double   scale;                            /* above 0; a normal fp32 number */
@@ -450,7 +450,7 @@ fd_status fd_kv_attend(const fd_kv* kv, const fd_kv_batch* batch, const fd_kv_at
  * ones with the largest weights (of equal ones the earlier; a NaN counts as the smallest), `keep` in all and in their order: row r
  * of the new cache is the old slot kept[r].  new_table: the pages they move to, either the same pages in the same order as the batch's table
  * (in place; then no other sequence may share them) or pages that no sequence of the batch uses; ceil(keep / page_size) columns suffice.  kept_dev: [batch][heads][keep], -1 behind the last.  new_len_dev:
- * [batch], may be kv_len.  weights_out_dev: the kept weights in their new order, zeros behind them up to kv_len; may be weights_in.
+ * [batch], may be kv_len.  weights_out_dev: the kept weights in their new order, zeros behind them up to kv_len; may be weights_in.  (Neither may lie partly over the other.)
  * A sequence whose length is out of range keeps its pages, its weights and its length, and has -1 in kept.  q_start is not read. */
 typedef struct {
     const float* weights_in_dev; float* weights_out_dev; int64_t weights_stride;

@@ -560,7 +560,7 @@ class KVCache:
     """Keys and values in pages: two pools [page, token in page, head, head_dim] (any strides with unit stride inside a head, so a pool laid
     out [page, head, token, head_dim] is passed transposed).  Calls run on the current stream and mirror the C entry points; workspaces are
     taken from the current stream's allocator for each call, so calls on several streams and captured graphs share nothing but the pools.  No graph is
-    built: tensors that require a gradient are refused outside torch.no_grad()."""
+    built: tensors that require a gradient are refused outside torch.no_grad().  A cache has to outlive its calls and the graphs that hold them."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         _need(isinstance(k_pages, torch.Tensor) and k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in (torch.bfloat16, torch.float16),

@@ -141,7 +141,8 @@ bool same(const fd_heads& a, const fd_heads& b) { return a.p_dev == b.p_dev && a
 }  // namespace
 
 // Few rows a sequence: as many CTAs as the GPU holds at once (two an SM), each with 64 tokens of a cache or more, share the caches evenly.  Else: the cache in parts of
-// at least two tiles of 128, as many as fill the GPU once if every sequence were as long as the longest, none longer than kPartTokens.
+// at least two tiles of 128, as many as fill the GPU once if every sequence were as long as the longest, none longer than kPartTokens (beyond kMaxSplits of them: as long as that
+// many parts are).
 Plan plan_attend(const fd_kv* kv, const fd_kv_batch* b, int q_heads, bool weights) {
     Plan p{};
     const int64_t heads = kv->d.heads, group = q_heads / heads, sms = kv->sm_count, live = std::min(b->batch, b->total_q);

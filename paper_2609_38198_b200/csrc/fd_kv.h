@@ -115,7 +115,7 @@ constexpr int kFewRows = 16;
 constexpr int kFewWarps = 4;             // warps of a CTA of that kernel; each goes through a quarter of what the CTA has of a cache
 constexpr int kMaxSplits = 1024;         // parts of a cache
 // Longest stretch of tokens that one accumulator of matrix products sums.  The tensor core truncates: of values of one sign, 1e-7 of the sum is lost with every 16
-// tokens (262144 tokens: 1.7e-3, nearly four half steps of fp16); parts are joined with rounding, so the loss ends at 2e-4.
+// tokens (262144 tokens: 1.7e-3, nearly four half steps of fp16; mma.sync the same); parts are joined with rounding, so the loss ends at 2.1e-4.
 constexpr int kPartTokens = 32768;
 
 // How the work of a call is cut, and what its workspace holds.

@@ -12,7 +12,7 @@
 //
 // Bounds: the tensor core (2 x 1024 clocks for two row tiles of 128 coordinates) and the MUFU (2 x 1024) could be busy all the time; what a pass takes is the chain
 // of one row tile -- scores ready, 600 clocks to read them and find the maximum, 1430 for 128 exponentials of one warp, 950 until the product and the next
-// scores are through -- about 3500 clocks while both row tiles take turns.  8192 new tokens over 16384: 1.56 ms, 1.06 PFLOP/s; without any exponentials 1.36
+// scores are through -- about 3500 clocks while both row tiles take turns.  8192 new tokens over 16384: 1.60 ms, 1.03 PFLOP/s; without any exponentials 1.36
 // ms (the power limit is near: a library product sustains 1.40 PFLOP/s).  Tried without gain: half a row a thread (16 warps, the maxima
 // exchanged: the same 3880 clocks under the profiler), an eighth of the exponentials as polynomials on the FMA pipe (1.57), a quarter (1.70), weights handed over
 // in one piece (1.64; in four pieces of 32 tokens the product starts on the first).

@@ -5,8 +5,8 @@
 // tokens of the CTA's part (32 where a row has 64 coordinates), keeps several chunks of keys and values in flight by TMA in a ring of its own (no barrier between warps),
 // multiplies with mma.sync m16n8k16 out of ldmatrix fragments and holds scores, weights and the 16 x D result in registers.  Two CTAs of four warps an SM
 // keep 192 KB in flight.  The caches of a batch are laid end to end in units of 64 tokens, and every CTA takes an equal stretch of them whatever the
-// lengths (which only the device knows): with a fixed number of parts a cache, two contexts of 131072 and 78000 tokens took 58 us, now 51.  Bytes bound it:
-// 64 sequences of 1400 to 4096 tokens 124 us a call, 5.8 TB/s.  A CTA's warps are joined in shared memory at the end of each cache it touches; a cache
+// lengths (which only the device knows): with a fixed number of parts a cache, two contexts of 131072 and 78000 tokens took 58 us, now 50.  Bytes bound it:
+// 64 sequences of 1400 to 4096 tokens 127 us a call, 5.7 TB/s.  A CTA's warps are joined in shared memory at the end of each cache it touches; a cache
 // that several CTAs share is joined by k_few_join.
 // With weights wanted, each row's scaled scores go to the workspace (4 bytes a row and token, beside 4 D bytes of keys and values), and k_few_join
 // turns them into weights once the norm is known: the keys are not read again.
