@@ -351,7 +351,8 @@ fd_status fd_unit_peaks(void* scratch_dev, size_t scratch_bytes, void* cuda_stre
  * live in pages of a pool.  They need no fd_ctx, take their stream per call and hold no device memory between calls.
  *
  * Element types: FD_BF16 and FD_FP16 (FD_FP32: fd_rotary only).  Scores, softmax statistics, sums and weights are fp32; a
- * softmax weight is rounded to the element type as an operand of the product with the values, results once at the end.
+ * softmax weight is rounded to the element type as an operand of the product with the values, results once at the end.  |scale q.k| up to 2^26 is
+ * covered: beyond, the steps of fp32 are too wide for a difference of scores to mean anything.
  * Heads: a tensor of heads is [token][head][head_dim] with unit stride inside a head; the other strides are free.
  * Pages: token t of a sequence is row t % page_size of the pool's page table[t / page_size]; page_size is a multiple of 8.
  * Lengths: sequence i has kv_len[i] tokens in the cache, the q_start[i + 1] - q_start[i] new ones among them, at the end; the new

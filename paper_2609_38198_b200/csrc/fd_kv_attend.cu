@@ -375,7 +375,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 const float top = max_nan(max_nan(mx[0], mx[1], mx[2]), mx[3], m);
                 const bool raise = !((top - m) * c <= kLazy<T>) && top != m;        // (first tile: from -inf; a NaN goes through)
                 if (__any_sync(~0u, raise)) {
-                    const float alpha = raise ? ex2f((m - top) * c) : 1.0f;
+                    const float alpha = raise ? rescale(m, top, c, kShift<T>) : 1.0f;
                     if (raise) m = top;
                     l *= alpha;
                     if (j > 0) {
@@ -393,7 +393,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         tmem_wait_st();
                     }
                 }
-                const float mc = m == -INFINITY ? 0.f : m * c - kShift<T>;
+                const float mc = held(m, c, kShift<T>);
                 const uint64_t cc = pair2(c, c), mm = pair2(-mc, -mc);
                 uint64_t sum[2] = {0, 0};
                 if (!kHold) tmem_ld32(s_addr, s[0]);
@@ -440,8 +440,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             const int64_t row = w.begin + token;
             const bool odd = num > 0 && *(volatile int*)&bars->odd;
             if (valid) {
-                if (a.splits > 1) a.part_lse[(split * (int64_t)a.batch.total_q + row) * a.q_heads + head] = empty ? -INFINITY : (m * c - kShift<T>) + log2f(l);
-                else if (a.lse) a.lse[row * a.q_heads + head] = empty ? -INFINITY : (float)((double)((m * c - kShift<T>) + log2f(l)) * 0.69314718055994530942);
+                if (a.splits > 1) a.part_lse[(split * (int64_t)a.batch.total_q + row) * a.q_heads + head] = empty ? -INFINITY : held(m, c, kShift<T>) + log2f(l);
+                else if (a.lse) a.lse[row * a.q_heads + head] = empty ? -INFINITY : (float)((double)(held(m, c, kShift<T>) + log2f(l)) * 0.69314718055994530942);
             }
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {

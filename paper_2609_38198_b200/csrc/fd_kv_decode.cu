@@ -221,7 +221,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
             float4* f = (float4*)a.folds + ((int64_t)(blockIdx.x * kWarpsFew + warp) * (D / 8 + 1)) * 32 + lane;
             if (!first) {
                 const float4 z = f[D / 8 * 32];
-                const float fa[2] = {z.x == m[0] ? 1.0f : ex2f((z.x - m[0]) * c), z.y == m[1] ? 1.0f : ex2f((z.y - m[1]) * c)};
+                const float fa[2] = {rescale(z.x, m[0], c, kShift<T>), rescale(z.y, m[1], c, kShift<T>)};
                 l[0] = fmaf(fa[0], z.z, l[0]);
                 l[1] = fmaf(fa[1], z.w, l[1]);
 #pragma unroll
@@ -292,7 +292,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                 for (int r = 0; r < 2; ++r) {
                     top[r] = max_nan(top[r], __shfl_xor_sync(~0u, top[r], 1));
                     top[r] = max_nan(top[r], __shfl_xor_sync(~0u, top[r], 2));
-                    const float f = top[r] == m[r] ? 1.0f : ex2f((m[r] - top[r]) * c);
+                    const float f = rescale(m[r], top[r], c, kShift<T>);
                     m[r] = top[r];
                     l[r] *= f;
 #pragma unroll
@@ -302,7 +302,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
             uint32_t p[NT / 2][4];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const float mc = m[r] == -INFINITY ? 0.f : m[r] * c - kShift<T>;
+                const float mc = held(m[r], c, kShift<T>);
                 float sum = 0.f;                     // (of the chunk first: beside one large weight every addition loses up to half a step of it)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -369,7 +369,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                 for (int k = 0; k < kWarpsFew; ++k) {
                     const float mk = s_m[k * 16 + row];
                     if (mk == -INFINITY) continue;
-                    const float f = mk == top ? 1.0f : ex2f((mk - top) * c);
+                    const float f = rescale(mk, top, c, kShift<T>);
                     const float4 y = *(const float4*)(s_o + (k * 16 + row) * D + d);
                     sum = fmaf(f, s_l[k * 16 + row], sum);
                     v[0] = fmaf(f, y.x, v[0]); v[1] = fmaf(f, y.y, v[1]); v[2] = fmaf(f, y.z, v[2]); v[3] = fmaf(f, y.w, v[3]);
@@ -395,7 +395,7 @@ k_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtenso
                     }
                 }
             }
-            const float lse2 = top == -INFINITY ? -INFINITY : (top * c - kShift<T>) + log2f(sum);
+            const float lse2 = top == -INFINITY ? -INFINITY : held(top, c, kShift<T>) + log2f(sum);
             if (cta0 != cta1) {
                 // (zeros, where the row sees nothing of the part: the join multiplies every part's result by a factor, which is 0 there)
                 if (d == 0) a.part_lse[slot * kFewRows + row] = lse2;

@@ -53,6 +53,14 @@ template <> struct Elem<__half> {
     static __device__ __forceinline__ float at(const void* p, int64_t i) { return __half2float(((const __half*)p)[i]); }
 };
 
+// What is taken off a score times c for the running maximum m: rounded up, so that no weight exceeds 2^kTop however large the scores, and the same number wherever sums made
+// with one maximum are brought to another or to a logarithm (m * c alone is off by half a step of scores that may be millions).
+__device__ __forceinline__ float held(float m, float c, float shift) { return m == -INFINITY ? 0.f : __fmaf_ru(m, c, -shift); }
+// Factor from sums made with maximum m to maximum top >= m.
+__device__ __forceinline__ float rescale(float m, float top, float c, float shift) {
+    return m == top ? 1.0f : m == -INFINITY ? 0.f : ex2f(held(m, c, shift) - held(top, c, shift));
+}
+
 // Which rows a CTA works on: sequence, its first token, what it may see.
 struct Work {
     int b, begin, count, n;           // sequence, its first row in q, its new tokens, its tokens in the cache

@@ -1143,3 +1143,22 @@ def test_evict_beyond_the_bounds_loses_nothing(fd, how, over):
         assert torch.equal(kept[1, h].long(), want)
         pg, r = p.where(1, torch.arange(100, device=DEV))
         assert torch.equal(p.k[pg, r, h].double(), old[1][0][want, h]) and torch.equal(w[1, h, :100], w0[1, h, want])
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("new", [1, 40])
+def test_attend_scores_of_millions(fd, dtype, new):
+    """Scores up to 2^28 (in powers of two), where the steps of fp32 are 16: one key far above the others, whose value the result is, whatever the largest score is
+    rounded to.  A weight is then at most 2^16 smaller than its place in the type says (2^10 or more), so it keeps its bits."""
+    for size in [300.0, 1000.0, 1500.0, 2000.0, 2500.0, 2900.0, *torch.linspace(3500, 4800, 14).tolist()]:
+        p = Pool(fd, int(size), [3000], [new], 1, 64, 16, dtype)
+        k, v = p.rows(0)
+        k[500], k[2900] = size / 2, size
+        p.set_rows(0, 0, k.to(dtype), v.to(dtype))
+        q = torch.full((new, 2, 64), size, dtype=dtype, device=DEV)
+        out, lse = p.cache.attend(p.batch, q, causal=False)
+        p.cache.synchronize()
+        want, half = v[2900], torch.finfo(dtype).eps / 2
+        assert ((out.double() - want).abs() <= (2 * half + 2.0 ** -19) * want.abs()).all(), size      # the weight and the result, rounded
+        top = float(64 * torch.tensor(size, dtype=dtype).double() ** 2 / 8)
+        assert (lse.double() - top).abs().max() <= 2.0 ** -21 * top
